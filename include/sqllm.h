@@ -70,8 +70,12 @@ typedef enum {
     SQLLM_ERR_NNZ = 5,    /* nnz < 0 or nnz >= 2^31                                       */
     SQLLM_ERR_BATCH = 6,  /* B outside 1..SQLLM_MAX_BATCH                                 */
     SQLLM_ERR_HIP = 7,    /* the HIP runtime reported an error (see the error string)     */
-    SQLLM_ERR_DEVICE = 8  /* the current device is not a gfx950 GPU                       */
+    SQLLM_ERR_DEVICE = 8, /* the current device is not a gfx950 GPU                       */
+    SQLLM_ERR_TYPE = 9    /* an element type is none of sqllm_type                        */
 } sqllm_status;
+
+/* element types of unpacked matrices, where an entry point takes one (everything else is fp16, see above) */
+typedef enum { SQLLM_F16 = 0, SQLLM_BF16 = 1, SQLLM_F32 = 2 } sqllm_type;
 
 #define SQLLM_MAX_BATCH 16
 #define SQLLM_MAX_N 28672 /* widest row a workgroup covers with one 2048-column slice per wave (14 waves) */
@@ -218,6 +222,36 @@ int sqllm_quantize_layer(int M, int N, int bits, int max_iter, const void* w, co
 int sqllm_quantize_layer_noalloc(int M, int N, int bits, int max_iter, const void* w, const void* sens,
                                  long long n_lo, long long n_hi, long long n_sens,
                                  void* qidx, void* lut, int* rowptr, int* cols, void* vals, int* iters, void* stream);
+
+/* ---- Microscaled 4-bit floating point: the format the matrix instructions of gfx950 multiply as it lies in memory ----
+ * A packed matrix of M rows and N columns is two device arrays.  Its rows are padded to P = 128 ceil(N / 128) columns.
+ *   codes   uint8 [M][P / 2]   column j of a row in the low (j even) or high (j odd) four bits of byte j / 2: bit 3 is the sign, bits 2..0 name
+ *                              the magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (two exponent bits, one fraction bit); columns N .. P - 1 hold zeros
+ *   scales  uint8 [M][P / 32]  one byte s per block of 32 neighbouring columns, the factor 2^(s - 127); 255 makes the block NaN
+ * codes are 16-byte aligned, scales 4-byte.  Unpacked matrices are row-major with a row stride ld (in elements, at least the number of columns), aligned
+ * to their element; 16-byte aligned rows are faster.  N is any number of columns from 1 to 2^31 - 128 unless stated otherwise, M any number of rows; M == 0 -> SQLLM_OK.
+ *
+ * sqllm_mx_bytes       the sizes of the two arrays in bytes (host pointers).
+ * sqllm_mx_quantize    packs w (`type`, [M][N], stride ldw).  With a the largest magnitude of a block its scale is 2^(floor(log2 a) - 2), not below 2^-127; each element is
+ *                      divided by it and rounded to the nearest magnitude (ties to the even code, 6 above 6); a block of zeros has s = 0.  A block that holds an Inf or
+ *                      NaN gets s = 255 and zero codes.  codes / scales take the matrix with its blocks along the rows; codes_t / scales_t its transpose (N rows of M
+ *                      columns, so blocks along the columns of w, and sizes sqllm_mx_bytes(N, M); then M must not exceed 2^31 - 128), as the products of a backward pass need it.
+ *                      Either pair may be NULL, not both; w is read once for both.  Rounding and scales are exact: the result is a pure function of w.
+ * sqllm_mx_dequantize  writes code * 2^(s - 127) as `type` to w_out [M][N], stride ldw; rounded once (fp16: beyond 65504 to Inf; exact where the type holds the value).
+ * sqllm_mx_gemv        y = W x (accumulate == 0) or y = fp16( fp32(y) + W x ): x fp16 [N][B], y fp16 [M][B], B = 1..16, N and the alignments of x and y as for sqllm_lut_gemv, so that
+ *                      sqllm_csr_spmv can add a sparse term of the same layer to y.  Products are exact, sums in fp32.
+ * sqllm_mx_gemm        y[t][i] = sum_j X[t][j] W[i][j] of two packed matrices: X has T rows, W has M, both N columns; y is `type` [T][M] with row stride ldy.  accumulate != 0 adds to
+ *                      what y holds (read as `type`, added in fp32).  Products are exact, sums in fp32; one rounding to `type`.  T == 0 -> SQLLM_OK.
+ *                      With X the tokens and W a layer this is its forward pass.  Backward, with dY [T][M]: dX = sqllm_mx_gemm of dY's rows and W's transpose, dW = of dY's transpose and X's transpose.
+ * Outputs must not overlap inputs.  Nothing but the named elements is written (rows of y and w_out keep what lies between their end and the next row).
+ * A NaN scale reaches every element of y whose sum it is part of.  Results do not depend on the launch: no atomics, fixed order of additions for a given shape.                     */
+int sqllm_mx_bytes(int M, int N, size_t* code_bytes, size_t* scale_bytes);
+int sqllm_mx_quantize(int M, int N, int type, const void* w, long long ldw, void* codes, void* scales,
+                      void* codes_t, void* scales_t, void* stream);
+int sqllm_mx_dequantize(int M, int N, int type, const void* codes, const void* scales, void* w_out, long long ldw, void* stream);
+int sqllm_mx_gemv(int M, int N, int B, const void* codes, const void* scales, const void* x, void* y, int accumulate, void* stream);
+int sqllm_mx_gemm(int T, int M, int N, int type, const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales,
+                  void* y, long long ldy, int accumulate, void* stream);
 
 /* Bytes the method moves for one matvec (indices + tables + CSR arrays + x + y); used for GB/s figures.  */
 long long sqllm_algorithmic_bytes(int M, int N, int bits, long long nnz, int B);

@@ -12,12 +12,14 @@ _lib = None
 
 OK = 0
 STATUS_NAMES = ["SQLLM_OK", "SQLLM_ERR_NULL", "SQLLM_ERR_BITS", "SQLLM_ERR_SHAPE", "SQLLM_ERR_ALIGN", "SQLLM_ERR_NNZ",
-                "SQLLM_ERR_BATCH", "SQLLM_ERR_HIP", "SQLLM_ERR_DEVICE"]
+                "SQLLM_ERR_BATCH", "SQLLM_ERR_HIP", "SQLLM_ERR_DEVICE", "SQLLM_ERR_TYPE"]
+TYPE_F16, TYPE_BF16, TYPE_F32 = 0, 1, 2          # sqllm_type
 
 EXPORTS = ["sqllm_lut_gemv", "sqllm_csr_spmv", "sqllm_dense_sparse_matvec", "sqllm_dense_sparse_matvec_multi", "sqllm_multi_launch_order", "sqllm_csr_spmv_rowwise",
            "sqllm_csr_plan_bytes", "sqllm_csr_plan_build",
            "sqllm_unpack_indices", "sqllm_dequantize", "sqllm_fp16_gemv", "sqllm_algorithmic_bytes",
            "sqllm_quantize_workspace_bytes", "sqllm_quantize_layer", "sqllm_quantize_layer_noalloc", "sqllm_extraction_counts",
+           "sqllm_mx_bytes", "sqllm_mx_quantize", "sqllm_mx_dequantize", "sqllm_mx_gemv", "sqllm_mx_gemm",
            "sqllm_last_error_string", "sqllm_status_string", "sqllm_version"]
 
 
@@ -61,6 +63,11 @@ def lib() -> ctypes.CDLL:
         L.sqllm_quantize_layer.argtypes = [i32, i32, i32, i32, vp, vp, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp]
         L.sqllm_quantize_layer_noalloc.argtypes = [i32, i32, i32, i32, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
         L.sqllm_extraction_counts.argtypes = [i32, i32, ctypes.c_double, ctypes.c_double, ctypes.POINTER(i64), ctypes.POINTER(i64), ctypes.POINTER(i64)]
+        L.sqllm_mx_bytes.argtypes = [i32, i32, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]
+        L.sqllm_mx_quantize.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, vp]
+        L.sqllm_mx_dequantize.argtypes = [i32, i32, i32, vp, vp, vp, i64, vp]
+        L.sqllm_mx_gemv.argtypes = [i32, i32, i32, vp, vp, vp, vp, i32, vp]
+        L.sqllm_mx_gemm.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i64, i32, vp]
         L.sqllm_last_error_string.restype = ctypes.c_char_p
         L.sqllm_status_string.argtypes = [i32]
         L.sqllm_status_string.restype = ctypes.c_char_p
@@ -221,6 +228,29 @@ def sqllm_extraction_counts(M, N, outlier_frac, sens_frac):
     n = [ctypes.c_longlong(0) for _ in range(3)]
     _check(lib().sqllm_extraction_counts(int(M), int(N), float(outlier_frac), float(sens_frac), *[ctypes.byref(v) for v in n]))
     return tuple(int(v.value) for v in n)
+
+
+def sqllm_mx_bytes(M, N):
+    """(bytes of the codes, bytes of the scales) of a packed matrix"""
+    c, s = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().sqllm_mx_bytes(int(M), int(N), ctypes.byref(c), ctypes.byref(s)))
+    return int(c.value), int(s.value)
+
+
+def sqllm_mx_quantize(M, N, type, w, ldw, codes, scales, codes_t=None, scales_t=None, stream=None):
+    _check(lib().sqllm_mx_quantize(M, N, type, _ptr(w), ldw, _ptr(codes), _ptr(scales), _ptr(codes_t), _ptr(scales_t), _stream(stream)))
+
+
+def sqllm_mx_dequantize(M, N, type, codes, scales, w_out, ldw, stream=None):
+    _check(lib().sqllm_mx_dequantize(M, N, type, _ptr(codes), _ptr(scales), _ptr(w_out), ldw, _stream(stream)))
+
+
+def sqllm_mx_gemv(M, N, B, codes, scales, x, y, accumulate=0, stream=None):
+    _check(lib().sqllm_mx_gemv(M, N, B, _ptr(codes), _ptr(scales), _ptr(x), _ptr(y), int(accumulate), _stream(stream)))
+
+
+def sqllm_mx_gemm(T, M, N, type, x_codes, x_scales, w_codes, w_scales, y, ldy, accumulate=0, stream=None):
+    _check(lib().sqllm_mx_gemm(T, M, N, type, _ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(y), ldy, int(accumulate), _stream(stream)))
 
 
 def sqllm_version() -> int:

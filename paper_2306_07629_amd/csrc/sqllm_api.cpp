@@ -10,6 +10,7 @@
 
 #include "sqllm.h"
 #include "sqllm_kernels.h"
+#include "sqllm_mx.h"
 
 namespace {
 
@@ -428,6 +429,91 @@ int sqllm_extraction_counts(int M, int N, double outlier_frac, double sens_frac,
     return SQLLM_OK;
 }
 
+// ---- microscaled 4-bit format
+namespace {
+
+int check_mx_columns(int N, const char* name) {
+    if (N <= 0 || N > sqllm::kMxMaxN) return fail(SQLLM_ERR_SHAPE, "%s = %d outside 1..%d", name, N, sqllm::kMxMaxN);
+    return SQLLM_OK;
+}
+
+int check_mx_rows(int M, const char* name) {
+    return M < 0 ? fail(SQLLM_ERR_SHAPE, "%s = %d is negative", name, M) : SQLLM_OK;
+}
+
+int check_mx_type(int type) {
+    if (type < SQLLM_F16 || type > SQLLM_F32) return fail(SQLLM_ERR_TYPE, "type = %d is none of sqllm_type", type);
+    return SQLLM_OK;
+}
+
+int check_mx_packed(const void* codes, const void* scales, const char* which) {
+    if (!codes || !scales) return fail(SQLLM_ERR_NULL, "codes / scales of %s must not be NULL", which);
+    if (misaligned(codes, 16) || misaligned(scales, 4)) return fail(SQLLM_ERR_ALIGN, "codes of %s must be 16-byte aligned, scales 4-byte", which);
+    return SQLLM_OK;
+}
+
+int check_mx_matrix(const void* p, long long ld, int columns, int type, const char* name) {
+    if (!p) return fail(SQLLM_ERR_NULL, "%s must not be NULL", name);
+    if (misaligned(p, sqllm::mx_type_size(type))) return fail(SQLLM_ERR_ALIGN, "%s must be aligned to its element", name);
+    if (ld < columns || ld > (1ll << 40)) return fail(SQLLM_ERR_SHAPE, "row stride %lld of %s: at least %d columns, at most 2^40", ld, name, columns);
+    return SQLLM_OK;
+}
+
+}  // namespace
+
+int sqllm_mx_bytes(int M, int N, size_t* code_bytes, size_t* scale_bytes) {
+    int st;
+    if ((st = check_mx_rows(M, "M")) || (st = check_mx_columns(N, "N"))) return st;
+    if (!code_bytes || !scale_bytes) return fail(SQLLM_ERR_NULL, "code_bytes / scale_bytes must not be NULL");
+    *code_bytes = (size_t)M * sqllm::mx_row_code_bytes(N);
+    *scale_bytes = (size_t)M * sqllm::mx_row_scale_bytes(N);
+    return SQLLM_OK;
+}
+
+int sqllm_mx_quantize(int M, int N, int type, const void* w, long long ldw, void* codes, void* scales, void* codes_t, void* scales_t, void* stream) {
+    int st;
+    if ((st = check_mx_type(type)) || (st = check_mx_rows(M, "M")) || (st = check_mx_columns(N, "N"))) return st;
+    const bool rows = codes || scales, columns = codes_t || scales_t;
+    if (M == 0) return SQLLM_OK;
+    if ((st = check_mx_matrix(w, ldw, N, type, "w"))) return st;
+    if (!rows && !columns) return fail(SQLLM_ERR_NULL, "neither codes / scales nor codes_t / scales_t are given");
+    if (rows && (st = check_mx_packed(codes, scales, "the rows"))) return st;
+    if (columns && ((st = check_mx_packed(codes_t, scales_t, "the transpose")) || (st = check_mx_columns(M, "M")))) return st;
+    if ((st = check_device())) return st;
+    const hipError_t e = sqllm::launch_mx_quantize({M, N, type, w, ldw, codes, scales, codes_t, scales_t}, static_cast<hipStream_t>(stream));
+    return e != hipSuccess ? hip_fail(e, "mx quantize launch") : SQLLM_OK;
+}
+
+int sqllm_mx_dequantize(int M, int N, int type, const void* codes, const void* scales, void* w_out, long long ldw, void* stream) {
+    int st;
+    if ((st = check_mx_type(type)) || (st = check_mx_rows(M, "M")) || (st = check_mx_columns(N, "N"))) return st;
+    if (M == 0) return SQLLM_OK;
+    if ((st = check_mx_packed(codes, scales, "the matrix")) || (st = check_mx_matrix(w_out, ldw, N, type, "w_out"))) return st;
+    if ((st = check_device())) return st;
+    const hipError_t e = sqllm::launch_mx_dequantize({M, N, type, codes, scales, w_out, ldw}, static_cast<hipStream_t>(stream));
+    return e != hipSuccess ? hip_fail(e, "mx dequantize launch") : SQLLM_OK;
+}
+
+int sqllm_mx_gemv(int M, int N, int B, const void* codes, const void* scales, const void* x, void* y, int accumulate, void* stream) {
+    int st;
+    if ((st = check_shape(M, N, B)) || (st = check_mx_packed(codes, scales, "the matrix")) || (st = check_xy(x, y))) return st;
+    if (M == 0) return SQLLM_OK;
+    if ((st = check_device())) return st;
+    const hipError_t e = sqllm::launch_mx_gemv({M, N, B, accumulate, codes, scales, x, y}, static_cast<hipStream_t>(stream));
+    return e != hipSuccess ? hip_fail(e, "mx gemv launch") : SQLLM_OK;
+}
+
+int sqllm_mx_gemm(int T, int M, int N, int type, const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales,
+                  void* y, long long ldy, int accumulate, void* stream) {
+    int st;
+    if ((st = check_mx_type(type)) || (st = check_mx_rows(T, "T")) || (st = check_mx_rows(M, "M")) || (st = check_mx_columns(N, "N"))) return st;
+    if (T == 0 || M == 0) return SQLLM_OK;
+    if ((st = check_mx_packed(x_codes, x_scales, "x")) || (st = check_mx_packed(w_codes, w_scales, "w")) || (st = check_mx_matrix(y, ldy, M, type, "y"))) return st;
+    if ((st = check_device())) return st;
+    const hipError_t e = sqllm::launch_mx_gemm({T, M, N, type, accumulate, x_codes, x_scales, w_codes, w_scales, y, ldy}, static_cast<hipStream_t>(stream));
+    return e != hipSuccess ? hip_fail(e, "mx gemm launch") : SQLLM_OK;
+}
+
 const char* sqllm_last_error_string(void) { return g_err; }
 
 const char* sqllm_status_string(int status) {
@@ -441,6 +527,7 @@ const char* sqllm_status_string(int status) {
         case SQLLM_ERR_BATCH: return "SQLLM_ERR_BATCH";
         case SQLLM_ERR_HIP: return "SQLLM_ERR_HIP";
         case SQLLM_ERR_DEVICE: return "SQLLM_ERR_DEVICE";
+        case SQLLM_ERR_TYPE: return "SQLLM_ERR_TYPE";
         default: return "SQLLM_ERR_UNKNOWN";
     }
 }

@@ -106,13 +106,206 @@ __global__ void __launch_bounds__(kGemmWaves * 64) mx_gemm_kernel(MxGemmArgs g, 
         }
 }
 
-hipError_t launch_mx_gemm(const MxGemmArgs& g, hipStream_t s) {
-    const int K = mx_padded(g.N), tiles_m = (int)(((long long)g.M + 63) / 64), tiles_t = (int)(((long long)g.T + 63) / 64);
-    const dim3 grid((unsigned)((long long)tiles_m * tiles_t));
-    if (g.type == SQLLM_F16) mx_gemm_kernel<SQLLM_F16><<<grid, kGemmWaves * 64, 0, s>>>(g, tiles_m, K);
-    else if (g.type == SQLLM_BF16) mx_gemm_kernel<SQLLM_BF16><<<grid, kGemmWaves * 64, 0, s>>>(g, tiles_m, K);
-    else mx_gemm_kernel<SQLLM_F32><<<grid, kGemmWaves * 64, 0, s>>>(g, tiles_m, K);
+// ---------------------------------------------------------------------------------------------- many rows on both sides
+constexpr int kTileRows = 256;                                       // of W and of X
+constexpr int kStageBytes = 2 * kTileRows * 64;                      // 128 columns of both
+constexpr int kScaleGroupBytes = 2 * kTileRows * 16;                 // scales of 512 columns of both
+
+__device__ __forceinline__ u32 chunk_swizzle(u32 row) { return ((row >> 1) ^ (row >> 3)) & 3u; }
+
+// What a lane holds of a result tile of 32 rows of W x 32 rows of X goes to y: four neighbouring elements of row t, four times.
+template <int TYPE, bool VEC>
+__device__ __forceinline__ void store_block(const MxGemmArgs& g, const f32x16& acc, long long m, long long t) {
+    typedef typename MxType<TYPE>::value value;
+    typedef value value4 __attribute__((ext_vector_type(4)));
+    if (t >= g.T) return;
+    value* y = static_cast<value*>(g.y) + t * g.ldy + m;
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        const long long left = g.M - (m + 2 * e);
+        if (VEC && left >= 4) {
+            value4* d = reinterpret_cast<value4*>(y + 2 * e);
+            value4 v;
+            if (g.accumulate) {
+                const value4 old = *d;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = (value)((float)old[i] + acc[e + i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = (value)acc[e + i];
+            }
+            *d = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) y[2 * e + i] = (value)(g.accumulate ? (float)y[2 * e + i] + acc[e + i] : acc[e + i]);
+        }
+    }
+}
+
+template <int TYPE, bool VEC>
+__global__ void __launch_bounds__(256, 1) mx_gemm_tile_kernel(MxGemmArgs g, int tiles_m, int tiles_t, int K) {
+    __shared__ __align__(16) char stage[2 * kStageBytes];
+    __shared__ __align__(16) char scale[2 * kScaleGroupBytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
+    const int n = tiles_m * tiles_t, xcd = blockIdx.x & 7, q8 = n >> 3, r8 = n & 7;
+    const int p = xcd * q8 + min(xcd, r8) + (int)(blockIdx.x >> 3);
+    const int per = 8 * tiles_t, grp = p / per, in = p % per, gsz = min(tiles_m - 8 * grp, 8);
+    const int tm = 8 * grp + in % gsz, tt = in / gsz;
+    const long long m0 = (long long)tm * kTileRows, t0 = (long long)tt * kTileRows;
+    const u32 cp = K / 2, sp = K / kMxBlock;
+    const int nst = K / 128;
+    // waves 0, 1 fetch the rows of W, 2, 3 those of X: 128 rows each, 16 rows of 64 bytes to an instruction
+    const bool mine_w = wave < 2;
+    const char* codes = static_cast<const char*>(mine_w ? g.w_codes : g.x_codes) + (size_t)(mine_w ? m0 : t0) * cp;
+    const char* scales = static_cast<const char*>(mine_w ? g.w_scales : g.x_scales) + (size_t)(mine_w ? m0 : t0) * sp;
+    const int last = (int)min((mine_w ? (long long)g.M - m0 : (long long)g.T - t0) - 1, (long long)kTileRows - 1);
+    u32 off[8], wr[8], soff[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const u32 row = 128 * (wave & 1) + 16 * i + (lane >> 2), rc = (u32)min((int)row, last);
+        off[i] = rc * cp + 16 * (lane & 3);
+        soff[i] = rc * sp;
+        wr[i] = wave * 8192 + 1024 * i + 64 * (lane >> 2) + 16 * ((lane & 3) ^ chunk_swizzle(row));
+    }
+    const int wm = wave & 1, wt = wave >> 1;
+    const u32 rd0 = r * 64 + 16 * ((2 * h) ^ chunk_swizzle(r)), rd1 = rd0 ^ 16;
+    const u32 rda = wm * 8192, rdb = 16384 + wt * 8192;
+    f32x16 acc[4][4] = {};
+    i32x4 a0[4], b0[4], a1[4], b1[4], pre[2][8];
+    u32 ua[4], ub[4], va[4], vb[4], spre[2][2];
+    auto fetch = [&](int s, i32x4 (&d)[8]) {
+        const char* base = codes + (size_t)min(s, nst - 1) * 64;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = *reinterpret_cast<const i32x4*>(base + off[i]);
+    };
+    auto put = [&](int s, const i32x4 (&d)[8]) {
+        char* b = stage + (s & 1) * kStageBytes;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *reinterpret_cast<i32x4*>(b + wr[i]) = d[i];
+    };
+    // quarter q of the scales of 512 columns: 32 rows of the wave's 128, four dwords each
+    auto fetch_scales = [&](int grp4, int q, u32 (&d)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int dw = 4 * grp4 + (lane & 3);
+            const u32 row = 128 * (wave & 1) + 32 * q + 16 * k + (lane >> 2), rc = (u32)min((int)row, last);
+            d[k] = *reinterpret_cast<const u32*>(scales + (size_t)(rc * sp + 4 * (u32)min(dw, nst - 1)));
+        }
+    };
+    auto put_scales = [&](int grp4, int q, const u32 (&d)[2]) {
+        char* b = scale + (grp4 & 1) * kScaleGroupBytes;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const u32 row = 32 * q + 16 * k + (lane >> 2);
+            *reinterpret_cast<u32*>(b + wave * 2048 + 16 * row + 4 * ((lane ^ (row >> 3)) & 3)) = 4 * grp4 + (lane & 3) < nst ? d[k] : 0u;
+        }
+    };
+    auto read = [&](int s, u32 rd, i32x4 (&a)[4], i32x4 (&b)[4]) {
+        const char* base = stage + (s & 1) * kStageBytes;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            a[f] = *reinterpret_cast<const i32x4*>(base + rda + rd + 2048 * f);
+            b[f] = *reinterpret_cast<const i32x4*>(base + rdb + rd + 2048 * f);
+        }
+    };
+    auto read_scales = [&](int s, u32 (&a)[4], u32 (&b)[4]) {
+        const char* base = scale + ((s >> 2) & 1) * kScaleGroupBytes + 16 * r + 4 * ((s ^ (r >> 3)) & 3) + 2 * h;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            a[f] = *reinterpret_cast<const uint16_t*>(base + wm * 2048 + 512 * f);
+            b[f] = *reinterpret_cast<const uint16_t*>(base + 4096 + wt * 2048 + 512 * f);
+        }
+    };
+    // before the first stage: stage 0 and the scales of the first 512 columns in LDS, stages 1 and 2 and the quarters to be written in stages 0 and 1 on the way
+    {
+        u32 s4[4][2];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) fetch_scales(0, q, s4[q]);
+        fetch(0, pre[0]);
+        put(0, pre[0]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) put_scales(0, q, s4[q]);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(1, pre[1]);
+        fetch_scales(1, 0, spre[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(2, pre[0]);
+        fetch_scales(1, 1, spre[1]);
+    }
+    __syncthreads();
+    read(0, rd0, a0, b0);
+    read_scales(0, ua, ub);
+    for (int s2 = 0; s2 < nst; s2 += 2) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int s = s2 + j;
+            put(s + 1, pre[1 - j]);
+            put_scales(s / 4 + 1, s & 3, spre[j]);
+            fetch(s + 3, pre[1 - j]);
+            fetch_scales((s + 2) / 4 + 1, (s + 2) & 3, spre[j]);
+            read(s, rd1, a1, b1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[i][k] = mma<0>(a0[i], b0[k], acc[i][k], ua[i], ub[k]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x200, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            read(s + 1, rd0, a0, b0);
+            read_scales(s + 1, va, vb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[i][k] = mma<1>(a1[i], b1[k], acc[i][k], ua[i], ub[k]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int f = 0; f < 4; ++f) { ua[f] = va[f]; ub[f] = vb[f]; }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) store_block<TYPE, VEC>(g, acc[i][k], m0 + 128 * wm + 32 * i + 4 * h, t0 + 128 * wt + 32 * k + r);
+}
+
+namespace {
+
+template <int TYPE>
+hipError_t gemm(const MxGemmArgs& g, hipStream_t s) {
+    const int K = mx_padded(g.N);
+    const long long big_m = ((long long)g.M + kTileRows - 1) / kTileRows, big_t = ((long long)g.T + kTileRows - 1) / kTileRows;
+    if (big_m * big_t >= 128 && K <= 1 << 24) {
+        const bool vec = (reinterpret_cast<uintptr_t>(g.y) & (4 * mx_type_size(TYPE) - 1)) == 0 && g.ldy % 4 == 0;
+        const dim3 grid((unsigned)(big_m * big_t));
+        if (vec) mx_gemm_tile_kernel<TYPE, true><<<grid, 256, 0, s>>>(g, (int)big_m, (int)big_t, K);
+        else mx_gemm_tile_kernel<TYPE, false><<<grid, 256, 0, s>>>(g, (int)big_m, (int)big_t, K);
+    } else {
+        const int tiles_m = (int)(((long long)g.M + 63) / 64), tiles_t = (int)(((long long)g.T + 63) / 64);
+        mx_gemm_kernel<TYPE><<<dim3((unsigned)((long long)tiles_m * tiles_t)), kGemmWaves * 64, 0, s>>>(g, tiles_m, K);
+    }
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mx_gemm(const MxGemmArgs& g, hipStream_t s) {
+    return g.type == SQLLM_F16 ? gemm<SQLLM_F16>(g, s) : g.type == SQLLM_BF16 ? gemm<SQLLM_BF16>(g, s) : gemm<SQLLM_F32>(g, s);
 }
 
 }  // namespace sqllm

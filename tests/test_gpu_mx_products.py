@@ -146,7 +146,30 @@ def test_gemm(T, M, N, kind):
         assert bool((big[:, :off] == 3.0).all()) and bool((big[:, off + M:] == 3.0).all())
 
 
-@pytest.mark.parametrize("T,M,N", [(33, 65, 300), (300, 270, 1152)])
+@pytest.mark.parametrize("T,M,N,kind", [(4101, 2050, 130, "f16"), (2048, 4096, 128, "bf16"), (2305, 3900, 1152, "bf16"), (4096, 2300, 640, "f32"), (1800, 5121, 2049, "f16"), (8200, 1030, 384, "f32"), (1, 40000, 256, "f16"),
+                                        (40000, 3, 130, "f32"), (260, 33000, 300, "bf16")])
+def test_gemm_of_many_rows(T, M, N, kind):
+    """enough rows on both sides, or on one, for the kernels that large products take; ragged ends in every direction"""
+    import torch
+    import paper_2306_07629_amd as sq
+    print(f"mx gemm {T}x{M}x{N} {kind}", flush=True)
+    rng = np.random.default_rng(T + M + N)
+    x, xv = packed(T, N, rng, 4, 124)
+    w, wv = packed(M, N, rng, 6, 119)
+    want, S = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    ld = M + 5
+    big = torch.full((T + 1, ld), 3.0, dtype=dtype_of(kind), device="cuda")
+    part = big[:T, :M]
+    sq.mx_gemm(x, w, y=part)
+    close(host(part), want, S, N, kind)
+    first = part.clone()
+    assert torch.equal(sq.mx_gemm(x, w, dtype_of(kind)), first)
+    sq.mx_gemm(x, w, y=part, accumulate=True)
+    close(host(part), host(first) + want, S, N, kind)
+    assert bool((big[:, M:] == 3.0).all()) and bool((big[T] == 3.0).all())
+
+
+@pytest.mark.parametrize("T,M,N", [(33, 65, 300), (300, 270, 1152), (2100, 4100, 640)])
 def test_gemm_ends_of_the_ranges(T, M, N):
     """NaN blocks reach their rows only; scales whose products leave fp16 or fp32 give infinities where the definition does"""
     import torch

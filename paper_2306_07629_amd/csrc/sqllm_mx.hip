@@ -6,6 +6,7 @@
 // what is above 6 becomes 6) with its sign.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <algorithm>
 
 #include "sqllm_mx.h"
 #include "sqllm_mx_device.h"
@@ -130,9 +131,106 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs 
 }
 
 // ---------------------------------------------------------------------------------------------- a few fp16 columns
+// One column: wave w of a workgroup owns columns [2048 w, 2048 w + 2048), lane l block 64 w + l of every row, and keeps the 32 activations of its
+// block in 16 registers while it walks down the workgroup's rows, four at a time with the next four requested.  The codes are converted
+// without their scale (every code is an fp16 number), so a block's sum is formed as for fp16 weights, and enters the row's sum times the scale in
+// fp32: no scale byte leaves a range.
+struct FourRows {
+    u32x4 codes[4];
+    u32 scale[4];
+};
+
+__device__ __forceinline__ float block_dot(const u32x4& c, const u32 (&x)[16]) {
+    float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const half2_t w0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 0), w1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 1);
+        const half2_t w2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 2), w3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 3);
+        a0 = __builtin_amdgcn_fdot2(w0, __builtin_bit_cast(half2_t, x[4 * d]), a0, false);
+        a1 = __builtin_amdgcn_fdot2(w1, __builtin_bit_cast(half2_t, x[4 * d + 1]), a1, false);
+        a0 = __builtin_amdgcn_fdot2(w2, __builtin_bit_cast(half2_t, x[4 * d + 2]), a0, false);
+        a1 = __builtin_amdgcn_fdot2(w3, __builtin_bit_cast(half2_t, x[4 * d + 3]), a1, false);
+    }
+    return a0 + a1;
+}
+
+// scale byte -> fp32 factor: 2^(byte - 127), NaN for 255
+__device__ __forceinline__ float scale_factor(u32 byte) {
+    const u32 bits = byte == 0u ? 0x00400000u : byte << 23;
+    return __uint_as_float(byte == 255u ? 0x7FC00000u : bits);
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+
+// Sums of four values over the wave; lanes 16 k .. 16 k + 15 end up with that of value 0, 2, 1, 3 for k = 0, 1, 2, 3.
+__device__ __forceinline__ float wave_sums(const float (&v)[4]) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[0]), __float_as_uint(v[1]), false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[2]), __float_as_uint(v[3]), false, false);
+    const float s01 = __uint_as_float(a[0]) + __uint_as_float(a[1]), s23 = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+    const auto c = __builtin_amdgcn_permlane16_swap(__float_as_uint(s01), __float_as_uint(s23), false, false);
+    float s = __uint_as_float(c[0]) + __uint_as_float(c[1]);
+    s = dpp_add<0xB1>(s);                                            // lane ^ 1
+    s = dpp_add<0x4E>(s);                                            // lane ^ 2
+    s = dpp_add<0x141>(s);                                           // half mirror: the other quad of the eight
+    return dpp_add<0x140>(s);                                        // mirror: the other eight
+}
+
+constexpr int kGemvMaxWaves = 14, kGemvMaxRows = 64;                 // rows of a workgroup
+
+__global__ void __launch_bounds__(kGemvMaxWaves * 64) mx_gemv_kernel(MxGemvArgs a, int rows) {
+    __shared__ float part[kGemvMaxWaves * kGemvMaxRows];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
+    const long long r0 = (long long)blockIdx.x * rows;
+    const int n = (int)min((long long)rows, a.M - r0);
+    const int nb = a.N / kMxBlock, block = 64 * wave + lane;
+    const bool inside = block < nb;
+    const int b = min(block, nb - 1);                                // surplus lanes read the last block and multiply with zeros
+    u32 x[16];
+    {
+        const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const half_t*>(a.x) + 32 * (size_t)b);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const u32x4 v = src[k];
+            x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
+        }
+    }
+    const char* codes = static_cast<const char*>(a.codes) + (size_t)r0 * (a.N / 2);
+    const uint8_t* scales = static_cast<const uint8_t*>(a.scales) + (size_t)r0 * nb;
+    auto load = [&](int r, FourRows& f) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = min(r + k, n - 1);
+            f.codes[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + (size_t)row * (a.N / 2)) + b);
+            f.scale[k] = __builtin_nontemporal_load(scales + (size_t)row * nb + b);
+        }
+    };
+    FourRows now, next;
+    load(0, now);
+    const int group = lane >> 4, slot = (group >> 1) | (group & 1) << 1;   // whose sum the lane holds after wave_sums
+    for (int r = 0; r < n; r += 4) {
+        if (r + 4 < n) load(r + 4, next);
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = inside ? block_dot(now.codes[k], x) * scale_factor(now.scale[k]) : 0.f;
+        const float s = wave_sums(v);
+        if ((lane & 15) == 0) part[(r + slot) * nw + wave] = s;
+        now = next;
+    }
+    __syncthreads();
+    if (tid < n) {
+        float s = 0.f;
+        for (int w = 0; w < nw; ++w) s += part[tid * nw + w];
+        half_t* y = static_cast<half_t*>(a.y) + r0 + tid;
+        *y = (half_t)(a.accumulate ? (float)*y + s : s);
+    }
+}
+
 // A wave to a row, lane l takes blocks l, l + 64, ...  The codes are converted without their scale (every code is an fp16 number), so the block's
 // sum is formed exactly as for fp16 weights, and enters the row's sum times the scale in fp32: no scale byte leaves the range.
-__global__ void __launch_bounds__(kThreads) mx_gemv_kernel(MxGemvArgs a) {
+__global__ void __launch_bounds__(kThreads) mx_gemv_columns_kernel(MxGemvArgs a) {
     const int lane = threadIdx.x & 63;
     const long long row = (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
     if (row >= a.M) return;
@@ -211,7 +309,14 @@ hipError_t launch_mx_dequantize(const MxDequantArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_mx_gemv(const MxGemvArgs& a, hipStream_t s) {
-    mx_gemv_kernel<<<dim3((unsigned)(((long long)a.M + 3) / 4)), kThreads, 0, s>>>(a);
+    if (a.B == 1) {
+        const int waves = (a.N + 2047) / 2048;
+        const int resident = 256 * (24 / waves);                     // workgroups that run side by side
+        const int rows = (int)std::min<long long>(kGemvMaxRows, std::max<long long>(1, ((long long)a.M + 4ll * resident - 1) / (4ll * resident)) * 4);
+        mx_gemv_kernel<<<dim3((unsigned)(((long long)a.M + rows - 1) / rows)), waves * 64, 0, s>>>(a, rows);
+    } else {
+        mx_gemv_columns_kernel<<<dim3((unsigned)(((long long)a.M + 3) / 4)), kThreads, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 

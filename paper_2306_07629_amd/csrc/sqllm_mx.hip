@@ -230,34 +230,141 @@ __global__ void __launch_bounds__(kGemvMaxWaves * 64) mx_gemv_kernel(MxGemvArgs 
 
 // A wave to a row, lane l takes blocks l, l + 64, ...  The codes are converted without their scale (every code is an fp16 number), so the block's
 // sum is formed exactly as for fp16 weights, and enters the row's sum times the scale in fp32: no scale byte leaves the range.
-__global__ void __launch_bounds__(kThreads) mx_gemv_columns_kernel(MxGemvArgs a) {
-    const int lane = threadIdx.x & 63;
-    const long long row = (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (row >= a.M) return;
-    const u32x4* codes = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.codes) + row * (size_t)(a.N / 2));
-    const uint8_t* scales = static_cast<const uint8_t*>(a.scales) + row * (size_t)(a.N / kMxBlock);
-    const half_t* x = static_cast<const half_t*>(a.x);
-    for (int t = 0; t < a.B; ++t) {
-        float sum = 0.f;
-        for (int b = lane; b < a.N / kMxBlock; b += 64) {
-            const u32x4 c = codes[b];
-            float part = 0.f;
+// Two to sixteen columns, on the matrix cores.  v_mfma_f32_16x16x32_f16 multiplies 16 rows of W x 32 columns by 32 rows of x x 16 columns: lane
+// (r, q) = (l % 16, l / 16) supplies eight neighbouring weights of row r and the same eight rows of x in column r, and keeps rows 4 q + e of column r.
+// A workgroup owns 16 RG rows; its waves deal the windows of 128 columns out among themselves.  Lane (r, q) holds block q of row r of a window
+// (16 bytes and one scale), converted with its scale to fp16, eights 0..3 for instructions 0..3; the window's 128 rows of x go through the wave's own
+// LDS, where they are padded to a multiple of four columns and read back transposed.  What columns past B hold reaches columns that are not stored.
+//
+// With its scale a code is an fp16 number for scale bytes 114 .. 140 (0.5 x 2^-13 .. 6 x 2^13).  A block with a byte of 60 or less adds less than
+// 28672 x 65504 x 6 x 2^(60 - 127) < 2^-32 to any result, far below half the smallest fp16 number, and becomes zeros.  Other bytes
+// (weights of other magnitudes, NaN) send the window to a slower form: one instruction per block with the codes alone, its result times the scale in fp32.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+constexpr int kWindow = 128, kBatchMaxWaves = 16;
+
+constexpr int batch_pitch(int B) { return (B + 3) / 4 * 4; }                     // halves of a row of x in LDS
+constexpr int batch_stage_bytes(int B) { return kWindow * batch_pitch(B) * 2 + (batch_pitch(B) < 16 ? 32 : 0); }   // short rows are read as if they had 16 columns
+static_assert(kBatchMaxWaves * batch_stage_bytes(16) <= 65536 && batch_stage_bytes(12) <= batch_stage_bytes(16), "the staging areas fit a launch's LDS");
+
+template <int B, int RG>
+__global__ void __launch_bounds__(kBatchMaxWaves * 64) mx_gemv_batch_kernel(MxGemvArgs a) {
+    constexpr int P = batch_pitch(B), L = (B + 3) / 4;               // 16-byte pieces of a window per lane
+    constexpr int PER = B % 4 == 0 ? 1 : B % 2 == 0 ? 4 : 8;          // LDS writes a piece takes
+    extern __shared__ __align__(16) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
+    const int r = lane & 15, q = lane >> 4;
+    const long long r0 = (long long)blockIdx.x * (16 * RG);
+    const int nwin = a.N / kWindow;
+    char* stage = smem + wave * batch_stage_bytes(B);
+    const u32x4* codes[RG];
+    const uint8_t* scales[RG];
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const u32 w[4] = {MxType<SQLLM_F16>::unpack<0>(c[d], 1.f), MxType<SQLLM_F16>::unpack<1>(c[d], 1.f), MxType<SQLLM_F16>::unpack<2>(c[d], 1.f), MxType<SQLLM_F16>::unpack<3>(c[d], 1.f)};
+    for (int g = 0; g < RG; ++g) {
+        const size_t row = (size_t)min(r0 + 16 * g + r, (long long)a.M - 1);
+        codes[g] = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.codes) + row * (a.N / 2)) + q;
+        scales[g] = static_cast<const uint8_t*>(a.scales) + row * (a.N / kMxBlock) + q;
+    }
+    const u32x4* x = static_cast<const u32x4*>(a.x);
+    int piece[L];
+    u32 at[L][PER];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const size_t j = (size_t)(32 * b + 8 * d + 2 * k) * a.B + t;
-                    part = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, w[k]), half2_t{x[j], x[j + a.B]}, part, false);
-                }
-            }
-            const u32 s = scales[b];
-            sum = __builtin_fmaf(s == 255u ? __builtin_nanf("") : __builtin_ldexpf(1.f, (int)s - 127), part, sum);
+    for (int i = 0; i < L; ++i) {
+        piece[i] = min(lane + 64 * i, 16 * B - 1);                   // surplus lanes repeat the last piece
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const u32 e = 8u * piece[i] + j * (8 / PER);
+            at[i][j] = 2 * (e / B * P + e % B);
+        }
+    }
+    u32x4 next_codes[RG], next_x[L];
+    u32 next_scale[RG];
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            next_codes[g] = __builtin_nontemporal_load(codes[g] + 4 * t);
+            next_scale[g] = __builtin_nontemporal_load(scales[g] + 4 * t);
         }
 #pragma unroll
-        for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
-        if (lane == 0) {
-            half_t* y = static_cast<half_t*>(a.y) + row * a.B + t;
+        for (int i = 0; i < L; ++i) next_x[i] = x[(size_t)t * (16 * B) + piece[i]];
+    };
+    f32x4 acc[RG] = {};
+    const u32 from = 2 * ((32 * q + (r >> 2)) * P + 4 * (r & 3));
+    if (wave < nwin) fetch(wave);
+    for (int t = wave; t < nwin; t += nw) {
+        u32x4 c[RG];
+        u32 s[RG];
+        bool plain = true;
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            c[g] = next_codes[g];
+            s[g] = next_scale[g];
+            plain = plain && (s[g] <= 60u || s[g] - 114u <= 26u);
+        }
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const u32x4 v = next_x[i];
+            if constexpr (PER == 1) {
+                *reinterpret_cast<u32x4*>(stage + at[i][0]) = v;
+            } else if constexpr (PER == 4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *reinterpret_cast<u32*>(stage + at[i][j]) = v[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) *reinterpret_cast<uint16_t*>(stage + at[i][j]) = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+            }
+        }
+        fetch(min(t + nw, nwin - 1));
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        half8_t xb[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + from + 16 * m * P));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + from + 16 * m * P + 8 * P));
+            xb[m] = __builtin_bit_cast(half8_t, (__attribute__((ext_vector_type(8))) short){lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w});
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        auto weights = [&](u32 codes8, float scale) {
+            const u32x4 w = {MxType<SQLLM_F16>::unpack<0>(codes8, scale), MxType<SQLLM_F16>::unpack<1>(codes8, scale), MxType<SQLLM_F16>::unpack<2>(codes8, scale),
+                             MxType<SQLLM_F16>::unpack<3>(codes8, scale)};
+            return __builtin_bit_cast(half8_t, w);
+        };
+        if (__builtin_amdgcn_ballot_w64(!plain) == 0) {
+#pragma unroll
+            for (int g = 0; g < RG; ++g)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(weights(c[g][m], mx_scale(s[g])), xb[m], acc[g], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int g = 0; g < RG; ++g)
+                for (int b = 0; b < 4; ++b) {                        // the lanes that hold block b of their rows; the others supply zeros
+                    f32x4 d = {};
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(weights(q == b ? c[g][m] : 0u, 1.f), xb[m], d, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[g][e] = __builtin_fmaf(scale_factor(__shfl(s[g], 16 * b + 4 * q + e)), d[e], acc[g][e]);
+                }
+        }
+    }
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(smem);                    // [wave][row][column]
+#pragma unroll
+    for (int g = 0; g < RG; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[wave * (RG * 256) + (16 * g + 4 * q + e) * 16 + r] = acc[g][e];
+    __syncthreads();
+    for (int i = tid; i < 16 * RG * 16; i += blockDim.x) {
+        const long long row = r0 + (i >> 4);
+        if ((i & 15) < B && row < a.M) {
+            float sum = 0.f;
+            for (int w = 0; w < nw; ++w) sum += part[w * (RG * 256) + i];
+            half_t* y = static_cast<half_t*>(a.y) + row * B + (i & 15);
             *y = (half_t)(a.accumulate ? (float)*y + sum : sum);
         }
     }
@@ -308,15 +415,35 @@ hipError_t launch_mx_dequantize(const MxDequantArgs& a, hipStream_t s) {
     return a.type == SQLLM_F16 ? dequantize<SQLLM_F16>(a, s) : a.type == SQLLM_BF16 ? dequantize<SQLLM_BF16>(a, s) : dequantize<SQLLM_F32>(a, s);
 }
 
-hipError_t launch_mx_gemv(const MxGemvArgs& a, hipStream_t s) {
-    if (a.B == 1) {
-        const int waves = (a.N + 2047) / 2048;
-        const int resident = 256 * (24 / waves);                     // workgroups that run side by side
-        const int rows = (int)std::min<long long>(kGemvMaxRows, std::max<long long>(1, ((long long)a.M + 4ll * resident - 1) / (4ll * resident)) * 4);
-        mx_gemv_kernel<<<dim3((unsigned)(((long long)a.M + rows - 1) / rows)), waves * 64, 0, s>>>(a, rows);
-    } else {
-        mx_gemv_columns_kernel<<<dim3((unsigned)(((long long)a.M + 3) / 4)), kThreads, 0, s>>>(a);
+namespace {
+
+template <int B, int RG>
+hipError_t gemv_batch(const MxGemvArgs& a, hipStream_t s) {
+    const long long groups = ((long long)a.M + 16 * RG - 1) / (16 * RG);
+    int waves = (int)std::min<long long>(kBatchMaxWaves, std::max<long long>(4, 4096 / groups));   // sixteen waves to a compute unit
+    waves = std::min(waves, std::max(1, a.N / kWindow));
+    const size_t lds = (size_t)waves * std::max(batch_stage_bytes(B), RG * 1024);
+    mx_gemv_batch_kernel<B, RG><<<dim3((unsigned)groups), waves * 64, lds, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int B>
+hipError_t gemv_batch(const MxGemvArgs& a, hipStream_t s) {
+    if constexpr (B > 1) {
+        if (a.B < B) return gemv_batch<B - 1>(a, s);
+        return a.M > 16 * 256 ? gemv_batch<B, 2>(a, s) : gemv_batch<B, 1>(a, s);
     }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_mx_gemv(const MxGemvArgs& a, hipStream_t s) {
+    if (a.B > 1) return gemv_batch<SQLLM_MAX_BATCH>(a, s);
+    const int waves = (a.N + 2047) / 2048;
+    const int resident = 256 * (24 / waves);                         // workgroups that run side by side
+    const int rows = (int)std::min<long long>(kGemvMaxRows, std::max<long long>(1, ((long long)a.M + 4ll * resident - 1) / (4ll * resident)) * 4);
+    mx_gemv_kernel<<<dim3((unsigned)(((long long)a.M + rows - 1) / rows)), waves * 64, 0, s>>>(a, rows);
     return hipGetLastError();
 }
 

@@ -131,27 +131,35 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs 
 }
 
 // ---------------------------------------------------------------------------------------------- a few fp16 columns
-// One column: wave w of a workgroup owns columns [2048 w, 2048 w + 2048), lane l block 64 w + l of every row, and keeps the 32 activations of its
-// block in 16 registers while it walks down the workgroup's rows, four at a time with the next four requested.  The codes are converted
+// One or two columns: wave w of a workgroup owns columns [2048 w, 2048 w + 2048) of W, lane l block 64 w + l of every row, and keeps the 32 rows of x of
+// its block in 16 registers per column of x while it walks down the workgroup's rows, R at a time with the next R requested.  The codes are converted
 // without their scale (every code is an fp16 number), so a block's sum is formed as for fp16 weights, and enters the row's sum times the scale in
 // fp32: no scale byte leaves a range.
-struct FourRows {
-    u32x4 codes[4];
-    u32 scale[4];
+template <int R>
+struct BlockRows {
+    u32x4 codes[R];
+    u32 scale[R];
 };
 
-__device__ __forceinline__ float block_dot(const u32x4& c, const u32 (&x)[16]) {
-    float a0 = 0.f, a1 = 0.f;
+template <int B>
+__device__ __forceinline__ void block_dot(const u32x4& c, const u32 (&x)[B][16], float (&sum)[B]) {
+    float odd[B];
+#pragma unroll
+    for (int t = 0; t < B; ++t) sum[t] = odd[t] = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
-        const half2_t w0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 0), w1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 1);
-        const half2_t w2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 2), w3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 3);
-        a0 = __builtin_amdgcn_fdot2(w0, __builtin_bit_cast(half2_t, x[4 * d]), a0, false);
-        a1 = __builtin_amdgcn_fdot2(w1, __builtin_bit_cast(half2_t, x[4 * d + 1]), a1, false);
-        a0 = __builtin_amdgcn_fdot2(w2, __builtin_bit_cast(half2_t, x[4 * d + 2]), a0, false);
-        a1 = __builtin_amdgcn_fdot2(w3, __builtin_bit_cast(half2_t, x[4 * d + 3]), a1, false);
+        const half2_t w[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 1),
+                              __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c[d], 1.f, 3)};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int t = 0; t < B; ++t) {
+                float& s = k & 1 ? odd[t] : sum[t];
+                s = __builtin_amdgcn_fdot2(w[k], __builtin_bit_cast(half2_t, x[t][4 * d + k]), s, false);
+            }
     }
-    return a0 + a1;
+#pragma unroll
+    for (int t = 0; t < B; ++t) sum[t] += odd[t];
 }
 
 // scale byte -> fp32 factor: 2^(byte - 127), NaN for 255
@@ -178,63 +186,86 @@ __device__ __forceinline__ float wave_sums(const float (&v)[4]) {
     return dpp_add<0x140>(s);                                        // mirror: the other eight
 }
 
-constexpr int kGemvMaxWaves = 14, kGemvMaxRows = 64;                 // rows of a workgroup
+constexpr int kGemvMaxWaves = 14, kGemvMaxSums = 128;                 // sums of a workgroup: rows x columns of x
+constexpr int kGemvColumns = 2;
 
+template <int B, int R>
 __global__ void __launch_bounds__(kGemvMaxWaves * 64) mx_gemv_kernel(MxGemvArgs a, int rows) {
-    __shared__ float part[kGemvMaxWaves * kGemvMaxRows];
+    __shared__ float part[kGemvMaxWaves * kGemvMaxSums];             // [row][column][wave]
+    constexpr int V = (R * B + 3) / 4 * 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
     const long long r0 = (long long)blockIdx.x * rows;
     const int n = (int)min((long long)rows, a.M - r0);
     const int nb = a.N / kMxBlock, block = 64 * wave + lane;
     const bool inside = block < nb;
     const int b = min(block, nb - 1);                                // surplus lanes read the last block and multiply with zeros
-    u32 x[16];
-    {
-        const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const half_t*>(a.x) + 32 * (size_t)b);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const u32x4 v = src[k];
-            x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
-        }
-    }
     const char* codes = static_cast<const char*>(a.codes) + (size_t)r0 * (a.N / 2);
     const uint8_t* scales = static_cast<const uint8_t*>(a.scales) + (size_t)r0 * nb;
-    auto load = [&](int r, FourRows& f) {
+    auto load = [&](int r, BlockRows<R>& f) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < R; ++k) {
             const int row = min(r + k, n - 1);
             f.codes[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + (size_t)row * (a.N / 2)) + b);
             f.scale[k] = __builtin_nontemporal_load(scales + (size_t)row * nb + b);
         }
     };
-    FourRows now, next;
+    u32 x[B][16];                                                    // rows 2 k, 2 k + 1 of column t as a pair
+    {
+        const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const half_t*>(a.x) + (size_t)(32 * B) * b);
+        u32 v[16 * B];
+#pragma unroll
+        for (int k = 0; k < 4 * B; ++k) {
+            const u32x4 t = src[k];
+            v[4 * k] = t.x; v[4 * k + 1] = t.y; v[4 * k + 2] = t.z; v[4 * k + 3] = t.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+#pragma unroll
+            for (int t = 0; t < B; ++t) {
+                const int lo = 2 * k * B + t, hi = lo + B;           // positions among the lane's halves
+                x[t][k] = B == 1 ? v[k] : __builtin_amdgcn_perm(v[hi / 2], v[lo / 2], (hi & 1 ? 0x07060000u : 0x05040000u) | (lo & 1 ? 0x0302u : 0x0100u));
+            }
+    }
+    BlockRows<R> now, next;
     load(0, now);
     const int group = lane >> 4, slot = (group >> 1) | (group & 1) << 1;   // whose sum the lane holds after wave_sums
-    for (int r = 0; r < n; r += 4) {
-        if (r + 4 < n) load(r + 4, next);
-        float v[4];
+    for (int r = 0; r < n; r += R) {
+        if (r + R < n) load(r + R, next);
+        float v[V];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = inside ? block_dot(now.codes[k], x) * scale_factor(now.scale[k]) : 0.f;
-        const float s = wave_sums(v);
-        if ((lane & 15) == 0) part[(r + slot) * nw + wave] = s;
+        for (int k = 0; k < R; ++k) {
+            float sum[B];
+            block_dot<B>(now.codes[k], x, sum);
+            const float f = scale_factor(now.scale[k]);
+#pragma unroll
+            for (int t = 0; t < B; ++t) v[k * B + t] = inside ? sum[t] * f : 0.f;
+        }
+#pragma unroll
+        for (int k = R * B; k < V; ++k) v[k] = 0.f;
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+            const float four[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
+            const float s = wave_sums(four);
+            if ((lane & 15) == 0 && k + slot < R * B) part[(r * B + k + slot) * nw + wave] = s;
+        }
         now = next;
     }
     __syncthreads();
-    if (tid < n) {
+    for (int i = tid; i < n * B; i += blockDim.x) {
         float s = 0.f;
-        for (int w = 0; w < nw; ++w) s += part[tid * nw + w];
-        half_t* y = static_cast<half_t*>(a.y) + r0 + tid;
+        for (int w = 0; w < nw; ++w) s += part[i * nw + w];
+        half_t* y = static_cast<half_t*>(a.y) + r0 * B + i;
         *y = (half_t)(a.accumulate ? (float)*y + s : s);
     }
 }
 
-// A wave to a row, lane l takes blocks l, l + 64, ...  The codes are converted without their scale (every code is an fp16 number), so the block's
-// sum is formed exactly as for fp16 weights, and enters the row's sum times the scale in fp32: no scale byte leaves the range.
-// Two to sixteen columns, on the matrix cores.  v_mfma_f32_16x16x32_f16 multiplies 16 rows of W x 32 columns by 32 rows of x x 16 columns: lane
+// Three to sixteen columns, on the matrix cores.  v_mfma_f32_16x16x32_f16 multiplies 16 rows of W x 32 columns by 32 rows of x x 16 columns: lane
 // (r, q) = (l % 16, l / 16) supplies eight neighbouring weights of row r and the same eight rows of x in column r, and keeps rows 4 q + e of column r.
-// A workgroup owns 16 RG rows; its waves deal the windows of 128 columns out among themselves.  Lane (r, q) holds block q of row r of a window
-// (16 bytes and one scale), converted with its scale to fp16, eights 0..3 for instructions 0..3; the window's 128 rows of x go through the wave's own
-// LDS, where they are padded to a multiple of four columns and read back transposed.  What columns past B hold reaches columns that are not stored.
+// A workgroup owns 16 G rows, each of its eight waves an equal share of the columns: n <= NS steps of 128 (in rounds of 8 x 8 steps where there are more).
+// Lane (r, q) takes block q of row r of every step, converted with its scale to fp16, eights 0..3 for instructions 0..3; the scales of a step are fetched
+// four lanes to a row and change lanes when they are used.  The wave's rows of x are read once per round, go through the wave's own LDS (padded there to a multiple of four columns) to
+// be transposed, and stay in 16 NS registers while the wave walks down the groups of 16 rows, RING of them ahead of itself with its requests.
+// What columns past B hold reaches columns that are not stored.
 //
 // With its scale a code is an fp16 number for scale bytes 114 .. 140 (0.5 x 2^-13 .. 6 x 2^13).  A block with a byte of 60 or less adds less than
 // 28672 x 65504 x 6 x 2^(60 - 127) < 2^-32 to any result, far below half the smallest fp16 number, and becomes zeros.  Other bytes
@@ -242,128 +273,162 @@ __global__ void __launch_bounds__(kGemvMaxWaves * 64) mx_gemv_kernel(MxGemvArgs 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-constexpr int kWindow = 128, kBatchMaxWaves = 16;
+constexpr int kBatchWaves = 8;
 
 constexpr int batch_pitch(int B) { return (B + 3) / 4 * 4; }                     // halves of a row of x in LDS
-constexpr int batch_stage_bytes(int B) { return kWindow * batch_pitch(B) * 2 + (batch_pitch(B) < 16 ? 32 : 0); }   // short rows are read as if they had 16 columns
-static_assert(kBatchMaxWaves * batch_stage_bytes(16) <= 65536 && batch_stage_bytes(12) <= batch_stage_bytes(16), "the staging areas fit a launch's LDS");
+constexpr int batch_stage_bytes(int B) { return 128 * batch_pitch(B) * 2 + (batch_pitch(B) < 16 ? 32 : 0); }   // short rows are read as if they had 16 columns
 
-template <int B, int RG>
-__global__ void __launch_bounds__(kBatchMaxWaves * 64) mx_gemv_batch_kernel(MxGemvArgs a) {
-    constexpr int P = batch_pitch(B), L = (B + 3) / 4;               // 16-byte pieces of a window per lane
-    constexpr int PER = B % 4 == 0 ? 1 : B % 2 == 0 ? 4 : 8;          // LDS writes a piece takes
-    extern __shared__ __align__(16) char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
-    const int r = lane & 15, q = lane >> 4;
-    const long long r0 = (long long)blockIdx.x * (16 * RG);
-    const int nwin = a.N / kWindow;
-    char* stage = smem + wave * batch_stage_bytes(B);
-    const u32x4* codes[RG];
-    const uint8_t* scales[RG];
+__device__ __forceinline__ void wave_fence() {                       // orders the LDS accesses of one wave
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <int NS>
+struct BatchCodes {                                                  // a lane's blocks of one group of rows
+    u32x4 c[NS];
+    u32 scale[(NS + 3) / 4];                                         // row lane / 4, scales of steps lane % 4, lane % 4 + 4
+};
+
+__device__ __forceinline__ half8_t fp16_weights(u32 codes, float scale) {
+    const u32x4 w = {MxType<SQLLM_F16>::unpack<0>(codes, scale), MxType<SQLLM_F16>::unpack<1>(codes, scale), MxType<SQLLM_F16>::unpack<2>(codes, scale),
+                     MxType<SQLLM_F16>::unpack<3>(codes, scale)};
+    return __builtin_bit_cast(half8_t, w);
+}
+
+// acc += 16 rows x 128 n columns of W times x
+template <int NS>
+__device__ __forceinline__ f32x4 batch_product(const BatchCodes<NS>& w, const half8_t (&xb)[NS][4], f32x4 acc, int n, int r, int q) {
+    u32 byte[NS];
+    bool plain = true;
 #pragma unroll
-    for (int g = 0; g < RG; ++g) {
-        const size_t row = (size_t)min(r0 + 16 * g + r, (long long)a.M - 1);
-        codes[g] = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.codes) + row * (a.N / 2)) + q;
-        scales[g] = static_cast<const uint8_t*>(a.scales) + row * (a.N / kMxBlock) + q;
+    for (int s = 0; s < NS; ++s) {
+        byte[s] = ((u32)__shfl((int)w.scale[s >> 2], 4 * r + (s & 3)) >> (8 * q)) & 255u;
+        plain = plain && (byte[s] <= 60u || byte[s] - 114u <= 26u);
     }
-    const u32x4* x = static_cast<const u32x4*>(a.x);
-    int piece[L];
-    u32 at[L][PER];
+    if (__builtin_amdgcn_ballot_w64(!plain) == 0) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-        piece[i] = min(lane + 64 * i, 16 * B - 1);                   // surplus lanes repeat the last piece
+        for (int s = 0; s < NS; ++s) {
+            if (s >= n) continue;                                    // uniform
+            const float scale = mx_scale(byte[s]);
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const u32 e = 8u * piece[i] + j * (8 / PER);
-            at[i][j] = 2 * (e / B * P + e % B);
+            for (int m = 0; m < 4; ++m) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp16_weights(w.c[s][m], scale), xb[s][m], acc, 0, 0, 0);
         }
-    }
-    u32x4 next_codes[RG], next_x[L];
-    u32 next_scale[RG];
-    auto fetch = [&](int t) {
+    } else {
 #pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            next_codes[g] = __builtin_nontemporal_load(codes[g] + 4 * t);
-            next_scale[g] = __builtin_nontemporal_load(scales[g] + 4 * t);
-        }
+        for (int s = 0; s < NS; ++s) {
+            if (s >= n) continue;
+#pragma unroll 1
+            for (int b = 0; b < 4; ++b) {                            // the lanes with q = b; the others supply zeros
+                f32x4 d = {};
 #pragma unroll
-        for (int i = 0; i < L; ++i) next_x[i] = x[(size_t)t * (16 * B) + piece[i]];
-    };
-    f32x4 acc[RG] = {};
-    const u32 from = 2 * ((32 * q + (r >> 2)) * P + 4 * (r & 3));
-    if (wave < nwin) fetch(wave);
-    for (int t = wave; t < nwin; t += nw) {
-        u32x4 c[RG];
-        u32 s[RG];
-        bool plain = true;
+                for (int m = 0; m < 4; ++m) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp16_weights(q == b ? w.c[s][m] : 0u, 1.f), xb[s][m], d, 0, 0, 0);
 #pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            c[g] = next_codes[g];
-            s[g] = next_scale[g];
-            plain = plain && (s[g] <= 60u || s[g] - 114u <= 26u);
-        }
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-            const u32x4 v = next_x[i];
-            if constexpr (PER == 1) {
-                *reinterpret_cast<u32x4*>(stage + at[i][0]) = v;
-            } else if constexpr (PER == 4) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *reinterpret_cast<u32*>(stage + at[i][j]) = v[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) *reinterpret_cast<uint16_t*>(stage + at[i][j]) = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+                for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(scale_factor(__shfl(byte[s], 16 * b + 4 * q + e)), d[e], acc[e]);
             }
         }
-        fetch(min(t + nw, nwin - 1));
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        half8_t xb[4];
+    }
+    return acc;
+}
+
+template <int B, int NS, int RING>
+__global__ void __launch_bounds__(kBatchWaves * 64, 2) mx_gemv_batch_kernel(MxGemvArgs a, int G, int share) {
+    constexpr int P = batch_pitch(B);
+    extern __shared__ __align__(16) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const long long r0 = (long long)blockIdx.x * (16 * G);
+    const int groups = (int)min((long long)G, (a.M - r0 + 15) / 16);
+    const int nb = a.N / kMxBlock, total = nb / 4;                   // blocks of a row, steps of a row (and dwords of its scales)
+    char* const stage = smem + wave * batch_stage_bytes(B);
+    float* const part = reinterpret_cast<float*>(smem + kBatchWaves * batch_stage_bytes(B)) + wave * (G * 256) + 64 * q + r;   // [wave][row][column]
+    for (int round = 0; round * kBatchWaves * share < total; ++round) {
+        const int first = min((round * kBatchWaves + wave) * share, total);   // the wave's first step
+        const int n = min(share, total - first);                     // uniform; may be 0
+        auto fetch = [&](int g, BatchCodes<NS>& d) {
+            const size_t row = (size_t)min(r0 + 16 * g + r, (long long)a.M - 1);
+            const u32x4* codes = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.codes) + row * (a.N / 2)) + 4 * first + q;
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + from + 16 * m * P));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + from + 16 * m * P + 8 * P));
-            xb[m] = __builtin_bit_cast(half8_t, (__attribute__((ext_vector_type(8))) short){lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w});
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        auto weights = [&](u32 codes8, float scale) {
-            const u32x4 w = {MxType<SQLLM_F16>::unpack<0>(codes8, scale), MxType<SQLLM_F16>::unpack<1>(codes8, scale), MxType<SQLLM_F16>::unpack<2>(codes8, scale),
-                             MxType<SQLLM_F16>::unpack<3>(codes8, scale)};
-            return __builtin_bit_cast(half8_t, w);
+            for (int s = 0; s < NS; ++s)
+                if (s < n) d.c[s] = codes[4 * s];
+            const size_t srow = (size_t)min(r0 + 16 * g + (lane >> 2), (long long)a.M - 1);
+            const u32* scales = reinterpret_cast<const u32*>(static_cast<const char*>(a.scales) + srow * nb);
+#pragma unroll
+            for (int k = 0; k < (NS + 3) / 4; ++k) d.scale[k] = scales[min(first + min(4 * k + (lane & 3), max(n, 1) - 1), total - 1)];
         };
-        if (__builtin_amdgcn_ballot_w64(!plain) == 0) {
+        BatchCodes<NS> ring[RING];
+        half8_t xb[NS][4];
+        {
+            // x: lane l fetches rows 2 l and 2 l + 1 of a step (B dwords)
+            const u32* x = static_cast<const u32*>(a.x) + (size_t)B * (64 * min(first, total - 1) + lane);
+            constexpr int C = B <= 4 ? NS : 4, EARLY = NS == 8 ? 1 : RING;   // steps of x requested ahead, groups of codes before x is in place: what 256 registers hold
+            u32 v[NS][B];
+            auto fetch_x = [&](int s) {
 #pragma unroll
-            for (int g = 0; g < RG; ++g)
+                for (int i = 0; i < B; ++i) v[s][i] = x[(size_t)B * (64 * min(s, max(n, 1) - 1)) + i];
+            };
 #pragma unroll
-                for (int m = 0; m < 4; ++m) acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(weights(c[g][m], mx_scale(s[g])), xb[m], acc[g], 0, 0, 0);
-        } else {
+            for (int s = 0; s < C && s < NS; ++s) fetch_x(s);
+            asm volatile("" ::: "memory");                           // keeps the requests in this order: x, whose transposition the codes outlast, then these
 #pragma unroll
-            for (int g = 0; g < RG; ++g)
-                for (int b = 0; b < 4; ++b) {                        // the lanes that hold block b of their rows; the others supply zeros
-                    f32x4 d = {};
+            for (int i = 0; i < EARLY; ++i)
+                if (i < groups) fetch(i, ring[i]);
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(weights(q == b ? c[g][m] : 0u, 1.f), xb[m], d, 0, 0, 0);
+            for (int s = 0; s < NS; ++s) {
+                asm volatile("" ::: "memory");
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[g][e] = __builtin_fmaf(scale_factor(__shfl(s[g], 16 * b + 4 * q + e)), d[e], acc[g][e]);
+                for (int h = 0; h < 2; ++h) {
+                    u32 row[P / 2];
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) {
+                        const int at = h * B + 2 * i;                // halves from the lane's first on
+                        row[i] = 2 * i >= B ? 0u : at % 2 == 0 ? v[s][at / 2] : __builtin_amdgcn_alignbyte(at / 2 + 1 < B ? v[s][at / 2 + 1] : 0u, v[s][at / 2], 2);
+                    }
+#pragma unroll
+                    for (int i = 0; i < P / 4; ++i) *reinterpret_cast<u32x2*>(stage + 2 * P * (2 * lane + h) + 8 * i) = u32x2{row[2 * i], row[2 * i + 1]};
                 }
+                wave_fence();
+                const u32 from = 2 * ((32 * q + (r >> 2)) * P + 4 * (r & 3));
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + from + 16 * m * P));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + from + 16 * m * P + 8 * P));
+                    xb[s][m] = __builtin_bit_cast(half8_t, (__attribute__((ext_vector_type(8))) short){lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w});
+                }
+                wave_fence();
+                if (s + C < NS) fetch_x(s + C);
+            }
+#pragma unroll
+            for (int i = EARLY; i < RING; ++i)
+                if (i < groups) fetch(i, ring[i]);
+        }
+#pragma unroll 1
+        for (int g0 = 0; g0 < groups; g0 += RING) {
+#pragma unroll
+            for (int j = 0; j < RING; ++j) {
+                const int g = g0 + j;
+                if (g < groups) {                                    // uniform
+                    float* out = part + 256 * g;
+                    f32x4 acc;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[e] = round == 0 ? 0.f : out[16 * e];
+                    acc = batch_product<NS>(ring[j], xb, acc, n, r, q);
+                    if (g + RING < groups) fetch(g + RING, ring[j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[16 * e] = acc[e];
+                }
+            }
         }
     }
     __syncthreads();
-    float* part = reinterpret_cast<float*>(smem);                    // [wave][row][column]
-#pragma unroll
-    for (int g = 0; g < RG; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part[wave * (RG * 256) + (16 * g + 4 * q + e) * 16 + r] = acc[g][e];
-    __syncthreads();
-    for (int i = tid; i < 16 * RG * 16; i += blockDim.x) {
+    const float* all = reinterpret_cast<const float*>(smem + kBatchWaves * batch_stage_bytes(B));
+    for (int i = tid; i < 16 * G * 16; i += kBatchWaves * 64) {
         const long long row = r0 + (i >> 4);
         if ((i & 15) < B && row < a.M) {
             float sum = 0.f;
-            for (int w = 0; w < nw; ++w) sum += part[w * (RG * 256) + i];
+#pragma unroll
+            for (int w = 0; w < kBatchWaves; ++w) sum += all[w * (G * 256) + i];
             half_t* y = static_cast<half_t*>(a.y) + row * B + (i & 15);
             *y = (half_t)(a.accumulate ? (float)*y + sum : sum);
         }
@@ -417,21 +482,36 @@ hipError_t launch_mx_dequantize(const MxDequantArgs& a, hipStream_t s) {
 
 namespace {
 
-template <int B, int RG>
-hipError_t gemv_batch(const MxGemvArgs& a, hipStream_t s) {
-    const long long groups = ((long long)a.M + 16 * RG - 1) / (16 * RG);
-    int waves = (int)std::min<long long>(kBatchMaxWaves, std::max<long long>(4, 4096 / groups));   // sixteen waves to a compute unit
-    waves = std::min(waves, std::max(1, a.N / kWindow));
-    const size_t lds = (size_t)waves * std::max(batch_stage_bytes(B), RG * 1024);
-    mx_gemv_batch_kernel<B, RG><<<dim3((unsigned)groups), waves * 64, lds, s>>>(a);
+template <int B, int R>
+hipError_t gemv_few(const MxGemvArgs& a, hipStream_t s) {
+    const int waves = (a.N + 2047) / 2048;
+    const long long resident = 256ll * (24 / waves);                 // workgroups that run side by side
+    const int most = kGemvMaxSums / B / R * R;
+    const int rows = (int)std::min<long long>(most, std::max<long long>(1, (a.M + R * resident - 1) / (R * resident)) * R);
+    mx_gemv_kernel<B, R><<<dim3((unsigned)(((long long)a.M + rows - 1) / rows)), waves * 64, 0, s>>>(a, rows);
+    return hipGetLastError();
+}
+
+template <int B, int NS, int RING>
+hipError_t gemv_batch(const MxGemvArgs& a, int share, hipStream_t s) {
+    // one workgroup to a compute unit, as long as the partial sums of its rows fit
+    const long long groups = ((long long)a.M + 15) / 16;
+    const int G = (int)std::min<long long>(8, (groups + 255) / 256);
+    const size_t lds = (size_t)kBatchWaves * (batch_stage_bytes(B) + G * 1024);
+    if (lds > 65536) {                                               // above what a launch gets without asking
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemv_batch_kernel<B, NS, RING>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    mx_gemv_batch_kernel<B, NS, RING><<<dim3((unsigned)((groups + G - 1) / G)), kBatchWaves * 64, lds, s>>>(a, G, share);
     return hipGetLastError();
 }
 
 template <int B>
 hipError_t gemv_batch(const MxGemvArgs& a, hipStream_t s) {
-    if constexpr (B > 1) {
+    if constexpr (B > kGemvColumns) {
         if (a.B < B) return gemv_batch<B - 1>(a, s);
-        return a.M > 16 * 256 ? gemv_batch<B, 2>(a, s) : gemv_batch<B, 1>(a, s);
+        const int steps = a.N / 128, rounds = (steps + 8 * kBatchWaves - 1) / (8 * kBatchWaves), share = (steps + rounds * kBatchWaves - 1) / (rounds * kBatchWaves);
+        return share <= 4 ? gemv_batch<B, 4, 4>(a, share, s) : share <= 6 ? gemv_batch<B, 6, 3>(a, share, s) : gemv_batch<B, 8, 2>(a, share, s);
     }
     return hipErrorInvalidValue;
 }
@@ -439,12 +519,11 @@ hipError_t gemv_batch(const MxGemvArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_mx_gemv(const MxGemvArgs& a, hipStream_t s) {
-    if (a.B > 1) return gemv_batch<SQLLM_MAX_BATCH>(a, s);
-    const int waves = (a.N + 2047) / 2048;
-    const int resident = 256 * (24 / waves);                         // workgroups that run side by side
-    const int rows = (int)std::min<long long>(kGemvMaxRows, std::max<long long>(1, ((long long)a.M + 4ll * resident - 1) / (4ll * resident)) * 4);
-    mx_gemv_kernel<<<dim3((unsigned)(((long long)a.M + rows - 1) / rows)), waves * 64, 0, s>>>(a, rows);
-    return hipGetLastError();
+    switch (a.B) {
+        case 1: return gemv_few<1, 4>(a, s);
+        case 2: return gemv_few<2, 4>(a, s);
+        default: return gemv_batch<SQLLM_MAX_BATCH>(a, s);
+    }
 }
 
 }  // namespace sqllm

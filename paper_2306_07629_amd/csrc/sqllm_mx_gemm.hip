@@ -7,6 +7,9 @@
 // s = 0..3, so its four scale bytes are one dword and its codes 64 neighbouring bytes.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "sqllm_mx.h"
 #include "sqllm_mx_device.h"
@@ -16,6 +19,7 @@ namespace sqllm {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 template <int S>
 __device__ __forceinline__ f32x16 mma(const i32x4& a, const i32x4& b, const f32x16& c, u32 sa, u32 sb) {
@@ -23,283 +27,427 @@ __device__ __forceinline__ f32x16 mma(const i32x4& a, const i32x4& b, const f32x
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, c, 4, 4, S, (int)sa, S, (int)sb);
 }
 
-// Four waves share a tile of 64 rows of W x 64 rows of X and deal its steps of 256 columns out among themselves; their sums meet in LDS.
-constexpr int kGemmWaves = 4;
+// ---------------------------------------------------------------------------------------------- few rows of X
+// The waves of a workgroup share a tile of 32 rows of W x 32 FT rows of X and deal its units of 256 columns out among themselves; their sums meet
+// in LDS.  A wave requests its next unit (eight lanes to the 128 bytes of a row) while it multiplies the present one, which changes lanes in the
+// wave's own part of LDS: chunk c of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor 16 neighbouring lanes, which read
+// the same chunk of different rows, meet in a bank.  Fetched by the lanes that use it, neighbouring lanes on different rows, every 16 bytes were an access of
+// the vector L1 of their own (33 x 11008 x 4096: 14.8 us).
+__device__ __forceinline__ u32 chunk_swizzle(u32 row) { return (row & 7u) ^ ((row >> 3) & 1u); }
 
-template <int TYPE>
-__global__ void __launch_bounds__(kGemmWaves * 64) mx_gemm_kernel(MxGemmArgs g, int tiles_m, int K) {
-    __shared__ float part[kGemmWaves][16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
-    const long long m0 = 64ll * (blockIdx.x % tiles_m), t0 = 64ll * (blockIdx.x / tiles_m);
+__device__ __forceinline__ void wave_fence() {                       // orders the LDS accesses of one wave
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+constexpr int kFewMaxWaves = 8;
+
+template <int TYPE, int FT>
+__global__ void __launch_bounds__(kFewMaxWaves * 64, 2) mx_gemm_few_kernel(MxGemmArgs g, int tiles_m, int K) {
+    constexpr int F = 1 + FT, kOwn = 32 * F * 128;                   // 32-row operands; bytes of a unit of them
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6, r = lane & 31, h = lane >> 5;
+    const long long m0 = 32ll * (blockIdx.x % tiles_m), t0 = (32ll * FT) * (blockIdx.x / tiles_m);
     const size_t cp = K / 2, sp = K / kMxBlock;
-    const char *ac[2], *bc[2], *as[2], *bs[2];
+    const int ndw = K / 128, units = (K + 255) / 256;
+    char* const own = lds + wave * kOwn;
+    const char *codes[F][4], *scales[F];                             // rows past the end repeat the last one; their results are not stored
 #pragma unroll
-    for (int f = 0; f < 2; ++f) {                                    // rows past the end repeat the last one; their results are not stored
-        const size_t m = min(m0 + 32 * f + r, (long long)g.M - 1), t = min(t0 + 32 * f + r, (long long)g.T - 1);
-        ac[f] = static_cast<const char*>(g.w_codes) + m * cp; as[f] = static_cast<const char*>(g.w_scales) + m * sp;
-        bc[f] = static_cast<const char*>(g.x_codes) + t * cp; bs[f] = static_cast<const char*>(g.x_scales) + t * sp;
+    for (int f = 0; f < F; ++f) {
+        const char* c = static_cast<const char*>(f == 0 ? g.w_codes : g.x_codes);
+        const char* s = static_cast<const char*>(f == 0 ? g.w_scales : g.x_scales);
+        const long long first = f == 0 ? m0 : t0 + 32 * (f - 1), last = (f == 0 ? g.M : g.T) - 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[f][i] = c + (size_t)min(first + 8 * i + (lane >> 3), last) * cp + 16 * (lane & 7);
+        scales[f] = s + (size_t)min(first + r, last) * sp;
     }
-    f32x16 acc[2][2] = {};
-    for (int k = 256 * wave; k + 256 <= K; k += 256 * kGemmWaves) {
-        i32x4 a[2][4], b[2][4];
-        u32 sa[2], sb[2];
+    i32x4 next[F][4];
+    u32 next_scale[F];
+    // K is a multiple of 128: the upper half of the last unit may lie behind the rows, and repeats the lower one with scales of 2^-127, whose products
+    // vanish against every fp32 number
+    auto fetch = [&](int u) {
+        const bool behind = 2 * u + 1 >= ndw;
+        const size_t at = (size_t)u * 128 - (behind && (lane & 4) ? 64 : 0);
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
+        for (int f = 0; f < F; ++f) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                a[f][s] = *reinterpret_cast<const i32x4*>(ac[f] + k / 2 + 64 * h + 16 * s);
-                b[f][s] = *reinterpret_cast<const i32x4*>(bc[f] + k / 2 + 64 * h + 16 * s);
-            }
-            sa[f] = *reinterpret_cast<const u32*>(as[f] + k / 32 + 4 * h);
-            sb[f] = *reinterpret_cast<const u32*>(bs[f] + k / 32 + 4 * h);
+            for (int i = 0; i < 4; ++i) next[f][i] = *reinterpret_cast<const i32x4*>(codes[f][i] + at);
+            next_scale[f] = *reinterpret_cast<const u32*>(scales[f] + 4 * (size_t)min(2 * u + h, ndw - 1));
         }
+    };
+    f32x16 acc[FT] = {};
+    if (wave < units) fetch(wave);
+    for (int u = wave; u < units; u += nw) {
+        u32 scale[F];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int f = 0; f < F; ++f) {
+            scale[f] = 2 * u + h < ndw ? next_scale[f] : 0u;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                acc[i][j] = mma<0>(a[i][0], b[j][0], acc[i][j], sa[i], sb[j]);
-                acc[i][j] = mma<1>(a[i][1], b[j][1], acc[i][j], sa[i], sb[j]);
-                acc[i][j] = mma<2>(a[i][2], b[j][2], acc[i][j], sa[i], sb[j]);
-                acc[i][j] = mma<3>(a[i][3], b[j][3], acc[i][j], sa[i], sb[j]);
+            for (int i = 0; i < 4; ++i) {
+                const u32 row = 8 * i + (lane >> 3);
+                *reinterpret_cast<i32x4*>(own + 4096 * f + 128 * row + 16 * ((lane & 7) ^ chunk_swizzle(row))) = next[f][i];
             }
-    }
-    if (K % 256 != 0 && (K / 256) % kGemmWaves == wave) {            // the last 128 columns: half h takes blocks 2 h + s
-        const int k = K - 128;
-        i32x4 a[2][2], b[2][2];
-        u32 sa[2], sb[2];
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                a[f][s] = *reinterpret_cast<const i32x4*>(ac[f] + k / 2 + 32 * h + 16 * s);
-                b[f][s] = *reinterpret_cast<const i32x4*>(bc[f] + k / 2 + 32 * h + 16 * s);
-            }
-            sa[f] = *reinterpret_cast<const u32*>(as[f] + k / 32) >> (16 * h);
-            sb[f] = *reinterpret_cast<const u32*>(bs[f] + k / 32) >> (16 * h);
         }
+        if (u + nw < units) fetch(u + nw);
+        wave_fence();
+        i32x4 op[F][4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int f = 0; f < F; ++f)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                acc[i][j] = mma<0>(a[i][0], b[j][0], acc[i][j], sa[i], sb[j]);
-                acc[i][j] = mma<1>(a[i][1], b[j][1], acc[i][j], sa[i], sb[j]);
-            }
+            for (int s = 0; s < 4; ++s) op[f][s] = *reinterpret_cast<const i32x4*>(own + 4096 * f + 128 * r + 16 * ((4 * h + s) ^ chunk_swizzle(r)));
+        wave_fence();
+#pragma unroll
+        for (int t = 0; t < FT; ++t) {
+            acc[t] = mma<0>(op[0][0], op[1 + t][0], acc[t], scale[0], scale[1 + t]);
+            acc[t] = mma<1>(op[0][1], op[1 + t][1], acc[t], scale[0], scale[1 + t]);
+            acc[t] = mma<2>(op[0][2], op[1 + t][2], acc[t], scale[0], scale[1 + t]);
+            acc[t] = mma<3>(op[0][3], op[1 + t][3], acc[t], scale[0], scale[1 + t]);
+        }
     }
+    // sums: [row of X][row of W], rows of 36 so that a wave's writes and the reads of rows spread over the banks
     typedef typename MxType<TYPE>::value value;
+    constexpr int kRow = 36;
+    static_assert(32 * kRow * 4 * FT <= kOwn, "a wave's sums fit its part");
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int t = 0; t < FT; ++t)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) part[wave][e][lane] = acc[i][j][e];
-            __syncthreads();
-#pragma unroll
-            for (int e = wave; e < 16; e += kGemmWaves) {
-                const float sum = (part[0][e][lane] + part[1][e][lane]) + (part[2][e][lane] + part[3][e][lane]);
-                const long long m = m0 + 32 * i + 8 * (e / 4) + 4 * h + e % 4, t = t0 + 32 * j + r;
-                if (m < g.M && t < g.T) {
-                    value* y = static_cast<value*>(g.y) + t * g.ldy + m;
-                    *y = (value)(g.accumulate ? (float)*y + sum : sum);
-                }
-            }
+        for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<f32x4*>(own + 4 * (kRow * (32 * t + r) + 4 * h + 2 * e)) = f32x4{acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]};
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * FT * 32; i += blockDim.x) {
+        const long long t = t0 + (i >> 5), m = m0 + (i & 31);
+        if (t < g.T && m < g.M) {
+            const char* s = lds + 4 * (kRow * (i >> 5) + (i & 31));
+            float sum = 0.f;
+            for (int w = 0; w < nw; ++w) sum += *reinterpret_cast<const float*>(s + w * kOwn);
+            value* y = static_cast<value*>(g.y) + t * g.ldy + m;
+            *y = (value)(g.accumulate ? (float)*y + sum : sum);
         }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- many rows on both sides
-constexpr int kTileRows = 256;                                       // of W and of X
-constexpr int kStageBytes = 2 * kTileRows * 64;                      // 128 columns of both
-constexpr int kScaleGroupBytes = 2 * kTileRows * 16;                 // scales of 512 columns of both
+// A workgroup of four waves makes a tile of R rows of W x R rows of X, R = 64 F, each wave a quarter of it in 16 F^2 accumulator registers: F = 4, one wave
+// to a SIMD, or F = 2, two workgroups to a compute unit.  Stages of 256 columns: a wave requests its share of the stage after next into 16 F registers (128
+// bytes of a row to eight lanes, whole cache lines), writes the next stage to the LDS buffer that is not being read, and feeds the matrix
+// instructions from the other; one barrier a stage.  Operands are read a step (64 columns) ahead.  Scales go the same way in groups of 512 columns.  Chunk c
+// (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor 16 neighbouring lanes, which read the same chunk of different
+// rows, meet in a bank.
+constexpr int kTileMinColumns = 512;                                 // a group of scales
 
-__device__ __forceinline__ u32 chunk_swizzle(u32 row) { return ((row >> 1) ^ (row >> 3)) & 3u; }
+template <int F>
+struct TileShape {
+    static constexpr int kRows = 64 * F;                             // of W and of X
+    static constexpr int kStageBytes = 2 * kRows * 128;              // 256 columns of both
+    static constexpr int kScaleGroupBytes = 2 * kRows * 16;          // scales of 512 columns of both
+    static constexpr int kPieces = 4 * F;                            // 16-byte pieces of a stage per lane
+    static constexpr int kPitch = kRows * 4 + 16;                    // of a row of sums in LDS: neighbouring rows four banks apart
+    static constexpr int kLds = 2 * kStageBytes + 2 * kScaleGroupBytes;
+    static_assert(kRows / 2 * kPitch <= kLds, "half a tile of sums fits");
+};
 
-// What a lane holds of a result tile of 32 rows of W x 32 rows of X goes to y: four neighbouring elements of row t, four times.
-template <int TYPE, bool VEC>
-__device__ __forceinline__ void store_block(const MxGemmArgs& g, const f32x16& acc, long long m, long long t) {
+typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+
+// Where tile p of the order lies.  Workgroups are handed to the eight XCDs in turn: each takes a contiguous range of the order, which goes through bands of
+// eight tiles of W, so that the tiles in flight on an XCD share rows in its L2.
+struct TileOrder {
+    int tiles_m, tiles_t, rows;
+    __device__ void at(int p, long long& m0, long long& t0) const {
+        const int per = 8 * tiles_t, band = p / per, in = p % per, wide = min(tiles_m - 8 * band, 8);
+        m0 = (long long)(8 * band + in % wide) * rows;
+        t0 = (long long)(in / wide) * rows;
+    }
+};
+
+// R / 2 rows of R sums in LDS to y, a quarter of them to each of four waves.
+template <int TYPE, int R, bool VEC>
+__device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds, int pitch, long long m0, long long t0, int wave, int lane) {
     typedef typename MxType<TYPE>::value value;
-    typedef value value4 __attribute__((ext_vector_type(4)));
-    if (t >= g.T) return;
-    value* y = static_cast<value*>(g.y) + t * g.ldy + m;
+    constexpr int E = 16 / sizeof(value), kLanes = R / E;     // elements of a 16-byte store, lanes to a row
+    if (VEC && m0 + R <= g.M) {
+        typedef value vec __attribute__((ext_vector_type(E)));
+        const int row0 = R / 8 * wave + lane / kLanes, col = E * (lane % kLanes);
+        auto rows = [&](auto add) {                                  // a loop for each: one that does both loses the kind of its stores
+#pragma unroll 4
+        for (int i = 0; i < R / 8; i += 64 / kLanes) {
+            const int row = row0 + i;
+            if (t0 + row >= g.T) continue;
+            vec* y = reinterpret_cast<vec*>(static_cast<value*>(g.y) + (t0 + row) * g.ldy + m0 + col);
+            const float* s = reinterpret_cast<const float*>(lds + row * pitch) + col;
+            float v[E];
 #pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-        const long long left = g.M - (m + 2 * e);
-        if (VEC && left >= 4) {
-            value4* d = reinterpret_cast<value4*>(y + 2 * e);
-            value4 v;
-            if (g.accumulate) {
-                const value4 old = *d;
+            for (int k = 0; k < E; k += 4) {
+                const f32x4 t = *reinterpret_cast<const f32x4*>(s + k);
+                v[k] = t.x; v[k + 1] = t.y; v[k + 2] = t.z; v[k + 3] = t.w;
+            }
+            vec out;
+            if constexpr (decltype(add)::value) {
+                const vec old = *y;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = (value)((float)old[i] + acc[e + i]);
+                for (int k = 0; k < E; ++k) out[k] = (value)((float)old[k] + v[k]);
+                *y = out;
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = (value)acc[e + i];
+                for (int k = 0; k < E; ++k) out[k] = (value)v[k];
+                __builtin_nontemporal_store(out, y);                 // 100 -> 84 us for 4096 x 16384 results of 1024 columns
             }
-            *d = v;
-        } else {
+        }
+        };
+        if (g.accumulate) rows(std::true_type{});
+        else rows(std::false_type{});
+    } else {
+        for (int i = 0; i < R / 8; ++i) {
+            const int row = R / 8 * wave + i;
+            if (t0 + row >= g.T) break;
+            value* y = static_cast<value*>(g.y) + (t0 + row) * g.ldy + m0;
+            const float* s = reinterpret_cast<const float*>(lds + row * pitch);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < left) y[2 * e + i] = (value)(g.accumulate ? (float)y[2 * e + i] + acc[e + i] : acc[e + i]);
+            for (int c = lane; c < R; c += 64)
+                if (m0 + c < g.M) y[c] = (value)(g.accumulate ? (float)y[c] + s[c] : s[c]);
         }
     }
 }
 
-template <int TYPE, bool VEC>
-__global__ void __launch_bounds__(256, 1) mx_gemm_tile_kernel(MxGemmArgs g, int tiles_m, int tiles_t, int K) {
-    __shared__ __align__(16) char stage[2 * kStageBytes];
-    __shared__ __align__(16) char scale[2 * kScaleGroupBytes];
+template <int TYPE, int F, bool VEC>
+__global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGemmArgs g, TileOrder order, int K) {
+    typedef TileShape<F> S;
+    constexpr int R = S::kRows, kStageBytes = S::kStageBytes, kScaleGroupBytes = S::kScaleGroupBytes, NP = S::kPieces;
+    __shared__ __align__(16) char lds[S::kLds];
+    char* const stage = lds;
+    char* const scale = lds + 2 * kStageBytes;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
-    const int n = tiles_m * tiles_t, xcd = blockIdx.x & 7, q8 = n >> 3, r8 = n & 7;
-    const int p = xcd * q8 + min(xcd, r8) + (int)(blockIdx.x >> 3);
-    const int per = 8 * tiles_t, grp = p / per, in = p % per, gsz = min(tiles_m - 8 * grp, 8);
-    const int tm = 8 * grp + in % gsz, tt = in / gsz;
-    const long long m0 = (long long)tm * kTileRows, t0 = (long long)tt * kTileRows;
+    // the workgroups of an XCD take its range of tiles in turn
+    const int tiles = order.tiles_m * order.tiles_t, xcd = blockIdx.x & 7, step = gridDim.x >> 3;
+    const int end = (int)((long long)tiles * (xcd + 1) >> 3);
+    int p = (int)((long long)tiles * xcd >> 3) + (int)(blockIdx.x >> 3);
+    if (p >= end) return;
+    long long m0, t0;
+    order.at(p, m0, t0);
     const u32 cp = K / 2, sp = K / kMxBlock;
-    const int nst = K / 128;
-    // waves 0, 1 fetch the rows of W, 2, 3 those of X: 128 rows each, 16 rows of 64 bytes to an instruction
+    const int ndw = K / 128, nst = (K + 255) / 256, ngr = (K + 511) / 512;   // dwords of scales of a row, stages, groups of scales
+    // waves 0, 1 fetch the rows of W, 2, 3 those of X: R / 2 each, eight of them to an instruction; rows past the end repeat the last one
     const bool mine_w = wave < 2;
-    const char* codes = static_cast<const char*>(mine_w ? g.w_codes : g.x_codes) + (size_t)(mine_w ? m0 : t0) * cp;
-    const char* scales = static_cast<const char*>(mine_w ? g.w_scales : g.x_scales) + (size_t)(mine_w ? m0 : t0) * sp;
-    const int last = (int)min((mine_w ? (long long)g.M - m0 : (long long)g.T - t0) - 1, (long long)kTileRows - 1);
-    u32 off[8], wr[8], soff[8];
+    const u32 row0 = R / 2 * (wave & 1);
+    const char *codes, *scales;
+    u32 off[NP], wr[2], soff[F / 2];
+    auto aim = [&]() {                                               // the fetches at the tile (m0, t0)
+        codes = static_cast<const char*>(mine_w ? g.w_codes : g.x_codes) + (size_t)(mine_w ? m0 : t0) * cp;
+        scales = static_cast<const char*>(mine_w ? g.w_scales : g.x_scales) + (size_t)(mine_w ? m0 : t0) * sp;
+        const int last = (int)min((mine_w ? (long long)g.M - m0 : (long long)g.T - t0) - 1, (long long)R - 1);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const u32 row = 128 * (wave & 1) + 16 * i + (lane >> 2), rc = (u32)min((int)row, last);
-        off[i] = rc * cp + 16 * (lane & 3);
-        soff[i] = rc * sp;
-        wr[i] = wave * 8192 + 1024 * i + 64 * (lane >> 2) + 16 * ((lane & 3) ^ chunk_swizzle(row));
-    }
+        for (int i = 0; i < NP; ++i) off[i] = (u32)min((int)(row0 + 8 * i + (lane >> 3)), last) * cp + 16 * (lane & 7);
+#pragma unroll
+        for (int i = 0; i < F / 2; ++i) soff[i] = (u32)min((int)(row0 + 64 * i + lane), last) * sp;
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) wr[i] = wave * (64 * R) + 128 * (8 * i + (lane >> 3)) + 16 * ((lane & 7) ^ chunk_swizzle(8 * i + (lane >> 3)));
     const int wm = wave & 1, wt = wave >> 1;
-    const u32 rd0 = r * 64 + 16 * ((2 * h) ^ chunk_swizzle(r)), rd1 = rd0 ^ 16;
-    const u32 rda = wm * 8192, rdb = 16384 + wt * 8192;
-    f32x16 acc[4][4] = {};
-    i32x4 a0[4], b0[4], a1[4], b1[4], pre[2][8];
-    u32 ua[4], ub[4], va[4], vb[4], spre[2][2];
-    auto fetch = [&](int s, i32x4 (&d)[8]) {
-        const char* base = codes + (size_t)min(s, nst - 1) * 64;
+    const u32 rda = wm * (64 * R) + r * 128, rdb = 128 * R + wt * (64 * R) + r * 128, swz = chunk_swizzle(r);
+    f32x16 acc[F][F];
+    i32x4 a0[F], b0[F], a1[F], b1[F], pre[NP];
+    u32 ua[F], ub[F], va[F], vb[F];
+    u32x4 spre[F / 2];
+    // K is a multiple of 128: the upper half of the last stage may lie behind the rows, and repeats the lower one with scales of 2^-127, whose products
+    // vanish against every fp32 number
+    auto fetch = [&](int st, int i) { pre[i] = *reinterpret_cast<const i32x4*>(codes + (size_t)min(st, nst - 1) * 128 + off[i] - ((lane & 4) && 2 * min(st, nst - 1) + 1 >= ndw ? 64 : 0)); };
+    auto put = [&](int st, int i) { *reinterpret_cast<i32x4*>(stage + (st & 1) * kStageBytes + 2048 * (i >> 1) + wr[i & 1]) = pre[i]; };
+    auto fetch_scales = [&](int gr) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = *reinterpret_cast<const i32x4*>(base + off[i]);
+        for (int i = 0; i < F / 2; ++i) spre[i] = *reinterpret_cast<const u32x4_a4*>(scales + (size_t)(soff[i] + 4 * (u32)min(4 * gr, ndw - 4)));
     };
-    auto put = [&](int s, const i32x4 (&d)[8]) {
-        char* b = stage + (s & 1) * kStageBytes;
+    auto put_scales = [&](int gr) {
+        char* b = scale + (gr & 1) * kScaleGroupBytes + wave * (8 * R);
+        const int over = max(4 * gr + 4 - ndw, 0);                   // dwords of the group behind the row's end: so much earlier it was fetched
+        const bool drop1 = over & 1, drop2 = over & 2, drop4 = over >= 4;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *reinterpret_cast<i32x4*>(b + wr[i]) = d[i];
-    };
-    // quarter q of the scales of 512 columns: 32 rows of the wave's 128, four dwords each
-    auto fetch_scales = [&](int grp4, int q, u32 (&d)[2]) {
+        for (int i = 0; i < F / 2; ++i) {
+            u32x4 v = spre[i];
+            v = u32x4{drop1 ? v.y : v.x, drop1 ? v.z : v.y, drop1 ? v.w : v.z, drop1 ? 0u : v.w};
+            v = u32x4{drop2 ? v.z : v.x, drop2 ? v.w : v.y, drop2 ? 0u : v.z, drop2 ? 0u : v.w};
+            v = u32x4{drop4 ? 0u : v.x, drop4 ? 0u : v.y, drop4 ? 0u : v.z, drop4 ? 0u : v.w};
+            const u32 row = 64 * i + lane;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int dw = 4 * grp4 + (lane & 3);
-            const u32 row = 128 * (wave & 1) + 32 * q + 16 * k + (lane >> 2), rc = (u32)min((int)row, last);
-            d[k] = *reinterpret_cast<const u32*>(scales + (size_t)(rc * sp + 4 * (u32)min(dw, nst - 1)));
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<u32*>(b + 16 * row + 4 * ((j ^ (row >> 3)) & 3)) = v[j];
         }
     };
-    auto put_scales = [&](int grp4, int q, const u32 (&d)[2]) {
-        char* b = scale + (grp4 & 1) * kScaleGroupBytes;
+    auto read = [&](int st, int s, i32x4 (&a)[F], i32x4 (&b)[F]) {
+        const char* base = stage + (st & 1) * kStageBytes + 16 * ((4 * h + s) ^ swz);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const u32 row = 32 * q + 16 * k + (lane >> 2);
-            *reinterpret_cast<u32*>(b + wave * 2048 + 16 * row + 4 * ((lane ^ (row >> 3)) & 3)) = 4 * grp4 + (lane & 3) < nst ? d[k] : 0u;
+        for (int f = 0; f < F; ++f) {
+            a[f] = *reinterpret_cast<const i32x4*>(base + rda + 4096 * f);
+            b[f] = *reinterpret_cast<const i32x4*>(base + rdb + 4096 * f);
         }
     };
-    auto read = [&](int s, u32 rd, i32x4 (&a)[4], i32x4 (&b)[4]) {
-        const char* base = stage + (s & 1) * kStageBytes;
+    auto read_scales = [&](int st) {
+        const char* base = scale + ((st >> 1) & 1) * kScaleGroupBytes + 16 * r + 4 * ((2 * (st & 1) + h) ^ ((r >> 3) & 3));
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            a[f] = *reinterpret_cast<const i32x4*>(base + rda + rd + 2048 * f);
-            b[f] = *reinterpret_cast<const i32x4*>(base + rdb + rd + 2048 * f);
+        for (int f = 0; f < F; ++f) {
+            va[f] = *reinterpret_cast<const u32*>(base + wm * (8 * R) + 512 * f);
+            vb[f] = *reinterpret_cast<const u32*>(base + 16 * R + wt * (8 * R) + 512 * f);
         }
     };
-    auto read_scales = [&](int s, u32 (&a)[4], u32 (&b)[4]) {
-        const char* base = scale + ((s >> 2) & 1) * kScaleGroupBytes + 16 * r + 4 * ((s ^ (r >> 3)) & 3) + 2 * h;
+    auto multiply = [&](auto s, const i32x4 (&a)[F], const i32x4 (&b)[F]) {
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            a[f] = *reinterpret_cast<const uint16_t*>(base + wm * 2048 + 512 * f);
-            b[f] = *reinterpret_cast<const uint16_t*>(base + 4096 + wt * 2048 + 512 * f);
-        }
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int k = 0; k < F; ++k) acc[i][k] = mma<decltype(s)::value>(a[i], b[k], acc[i][k], ua[i], ub[k]);
     };
-    // before the first stage: stage 0 and the scales of the first 512 columns in LDS, stages 1 and 2 and the quarters to be written in stages 0 and 1 on the way
-    {
-        u32 s4[4][2];
+    auto one_stage = [&](int st, auto odd) {
+        constexpr bool kOdd = decltype(odd)::value;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) fetch_scales(0, q, s4[q]);
-        fetch(0, pre[0]);
-        put(0, pre[0]);
+        for (int f = 0; f < F; ++f) { ua[f] = va[f]; ub[f] = vb[f]; }
+        // the pieces of the next stage go to LDS and those of the one after are requested in the first three steps
+        read(st, 1, a1, b1);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) put_scales(0, q, s4[q]);
+        for (int i = 0; i < 3 * F / 2; ++i) { put(st + 1, i); fetch(st + 2, i); }
+        multiply(std::integral_constant<int, 0>{}, a0, b0);
+#pragma unroll
+        for (int i = 0; i < (F == 4 ? 8 : 2); ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
-        fetch(1, pre[1]);
-        fetch_scales(1, 0, spre[0]);
+        read(st, 2, a0, b0);
+#pragma unroll
+        for (int i = 3 * F / 2; i < 3 * F; ++i) { put(st + 1, i); fetch(st + 2, i); }
+        multiply(std::integral_constant<int, 1>{}, a1, b1);
+#pragma unroll
+        for (int i = 0; i < (F == 4 ? 8 : 2); ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        }
         __builtin_amdgcn_sched_barrier(0);
-        fetch(2, pre[0]);
-        fetch_scales(1, 1, spre[1]);
-    }
-    __syncthreads();
-    read(0, rd0, a0, b0);
-    read_scales(0, ua, ub);
-    for (int s2 = 0; s2 < nst; s2 += 2) {
+        read(st, 3, a1, b1);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int s = s2 + j;
-            put(s + 1, pre[1 - j]);
-            put_scales(s / 4 + 1, s & 3, spre[j]);
-            fetch(s + 3, pre[1 - j]);
-            fetch_scales((s + 2) / 4 + 1, (s + 2) & 3, spre[j]);
-            read(s, rd1, a1, b1);
+        for (int i = 3 * F; i < NP; ++i) { put(st + 1, i); fetch(st + 2, i); }
+        if (kOdd) put_scales((st >> 1) + 1);
+        else fetch_scales((st >> 1) + 1);
+        multiply(std::integral_constant<int, 2>{}, a0, b0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < (F == 4 ? 8 : 2); ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 2);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
+            __builtin_amdgcn_sched_group_barrier(0x200, kOdd ? 2 : 1, 2);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 2);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        read(st + 1, 0, a0, b0);
+        read_scales(st + 1);
+        multiply(std::integral_constant<int, 3>{}, a1, b1);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) acc[i][k] = mma<0>(a0[i], b0[k], acc[i][k], ua[i], ub[k]);
+        for (int i = 0; i < (F == 4 ? 8 : 2); ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 3);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 3);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto request = [&]() {                                           // the first stage and scales of the tile aimed at
+        fetch_scales(0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x200, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < NP; ++i) fetch(0, i);
+    };
+    aim();
+    request();
+    while (true) {
+        put_scales(0);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) put(0, i);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) fetch(1, i);
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int k = 0; k < F; ++k) acc[i][k] = f32x16{};
+        __syncthreads();
+        read(0, 0, a0, b0);
+        read_scales(0);
+        for (int st = 0; st < nst; st += 2) {                        // an odd number of stages is filled up by one whose scales are all 2^-127
+            one_stage(st, std::false_type{});
+            one_stage(st + 1, std::true_type{});
+        }
+        // The next tile's first stage is requested before this one's result goes out.
+        const long long m_out = m0, t_out = t0;
+        p += step;
+        const bool more = p < end;
+        if (more) {
+            order.at(p, m0, t0);
+            aim();
+            request();
+        }
+        // Through LDS, half the rows of X at a time, so that whole lines of y are written (eight bytes of sixteen rows to an instruction, straight
+        // from the accumulators, kept the L2 busy with requests for as long as 64 stages of a tile take).
+        constexpr int kPitch = S::kPitch;
+        for (int half = 0; half < 2; ++half) {
             __syncthreads();
-            __builtin_amdgcn_sched_barrier(0);
-            read(s + 1, rd0, a0, b0);
-            read_scales(s + 1, va, vb);
+            if (wt == half) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < F; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) acc[i][k] = mma<1>(a1[i], b1[k], acc[i][k], ua[i], ub[k]);
+                    for (int k = 0; k < F; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-                __builtin_amdgcn_sched_group_barrier(0x008, 2, 1);
+                        for (int e = 0; e < 16; e += 4)
+                            *reinterpret_cast<f32x4*>(lds + (32 * k + r) * kPitch + 4 * (R / 2 * wm + 32 * i + 4 * h + 2 * e)) = f32x4{acc[i][k][e], acc[i][k][e + 1], acc[i][k][e + 2], acc[i][k][e + 3]};
             }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int f = 0; f < 4; ++f) { ua[f] = va[f]; ub[f] = vb[f]; }
+            __syncthreads();
+            store_rows<TYPE, R, VEC>(g, lds, kPitch, m_out, t_out + R / 2 * half, wave, lane);
         }
+        if (!more) break;
+        __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) store_block<TYPE, VEC>(g, acc[i][k], m0 + 128 * wm + 32 * i + 4 * h, t0 + 128 * wt + 32 * k + r);
 }
 
 namespace {
 
+template <int TYPE, int F>
+hipError_t gemm_tiles(const MxGemmArgs& g, int K, hipStream_t s) {
+    constexpr int R = TileShape<F>::kRows;
+    const TileOrder order = {(int)(((long long)g.M + R - 1) / R), (int)(((long long)g.T + R - 1) / R), R};
+    const unsigned grid = F == 4 ? 256 : 512;                        // one workgroup to a compute unit, or two
+    const bool vec = (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy * mx_type_size(TYPE) % 16 == 0;
+    if (vec) mx_gemm_tile_kernel<TYPE, F, true><<<grid, 256, 0, s>>>(g, order, K);
+    else mx_gemm_tile_kernel<TYPE, F, false><<<grid, 256, 0, s>>>(g, order, K);
+    return hipGetLastError();
+}
+
+template <int TYPE, int FT>
+hipError_t gemm_few(const MxGemmArgs& g, int K, hipStream_t s) {
+    const long long tiles_m = ((long long)g.M + 31) / 32, tiles = tiles_m * (((long long)g.T + 32 * FT - 1) / (32 * FT));
+    const int waves = std::min(tiles > 256 ? 4 : 8, (K + 255) / 256);
+    const size_t lds = (size_t)waves * (1 + FT) * 4096;
+    if (lds > 65536) {                                               // above what a launch gets without asking
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemm_few_kernel<TYPE, FT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    mx_gemm_few_kernel<TYPE, FT><<<dim3((unsigned)tiles), waves * 64, lds, s>>>(g, (int)tiles_m, K);
+    return hipGetLastError();
+}
+
+// Which kernel: the one whose estimate is lowest.  An estimate is a fixed part and a part per 1024 columns (k) for each round of tiles over the compute units,
+// fitted to measured times: 4096 x 16384 results of 1024 / 8192 columns take 81 / 326 us with tiles of 256 and 79 / 375 with 128, 2047 x 4096 of
+// 11008 83 and 67, 301 x 5120 of 5120 42 and 17 (22 with few rows), 128 x 4096 of 11008 29 with 128 and 15 with few rows, 33 x 11008 of 4096 13.4 and 12.
 template <int TYPE>
 hipError_t gemm(const MxGemmArgs& g, hipStream_t s) {
     const int K = mx_padded(g.N);
-    const long long big_m = ((long long)g.M + kTileRows - 1) / kTileRows, big_t = ((long long)g.T + kTileRows - 1) / kTileRows;
-    if (big_m * big_t >= 128 && K <= 1 << 24) {
-        const bool vec = (reinterpret_cast<uintptr_t>(g.y) & (4 * mx_type_size(TYPE) - 1)) == 0 && g.ldy % 4 == 0;
-        const dim3 grid((unsigned)(big_m * big_t));
-        if (vec) mx_gemm_tile_kernel<TYPE, true><<<grid, 256, 0, s>>>(g, (int)big_m, (int)big_t, K);
-        else mx_gemm_tile_kernel<TYPE, false><<<grid, 256, 0, s>>>(g, (int)big_m, (int)big_t, K);
-    } else {
-        const int tiles_m = (int)(((long long)g.M + 63) / 64), tiles_t = (int)(((long long)g.T + 63) / 64);
-        mx_gemm_kernel<TYPE><<<dim3((unsigned)((long long)tiles_m * tiles_t)), kGemmWaves * 64, 0, s>>>(g, tiles_m, K);
-    }
-    return hipGetLastError();
+    const double k = K / 1024.0;
+    auto tiles = [&](int m, int t) { return (double)((((long long)g.M + m - 1) / m) * (((long long)g.T + t - 1) / t)); };
+    const double tiles2 = tiles(128, 128);
+    const double cost4 = std::ceil(tiles(256, 256) / 256) * (12.6 + 7.6 * k);
+    const double cost2 = tiles2 <= 256 ? 4.5 + 2.4 * k : std::ceil(tiles2 / 512) * (4.2 + 5.2 * k);
+    const double few = 6.7 + 0.0039 * tiles(32, g.T <= 32 ? 32 : 64) * k;
+    // kTileMinColumns: a group of scales is fetched whole; 2^24: offsets inside a tile are 32 bits
+    if (K >= kTileMinColumns && K <= 1 << 24 && std::min(cost4, cost2) < few) return cost4 < cost2 ? gemm_tiles<TYPE, 4>(g, K, s) : gemm_tiles<TYPE, 2>(g, K, s);
+    return g.T <= 32 ? gemm_few<TYPE, 1>(g, K, s) : gemm_few<TYPE, 2>(g, K, s);
 }
 
 }  // namespace

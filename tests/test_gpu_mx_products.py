@@ -147,7 +147,7 @@ def test_gemm(T, M, N, kind):
 
 
 @pytest.mark.parametrize("T,M,N,kind", [(4101, 2050, 130, "f16"), (2048, 4096, 128, "bf16"), (2305, 3900, 1152, "bf16"), (4096, 2300, 640, "f32"), (1800, 5121, 2049, "f16"), (8200, 1030, 384, "f32"), (1, 40000, 256, "f16"),
-                                        (40000, 3, 130, "f32"), (260, 33000, 300, "bf16")])
+                                        (40000, 3, 130, "f32"), (260, 33000, 300, "bf16"), (2040, 8190, 4100, "f32"), (2048, 8192, 4096, "bf16")])
 def test_gemm_of_many_rows(T, M, N, kind):
     """enough rows on both sides, or on one, for the kernels that large products take; ragged ends in every direction"""
     import torch

@@ -28,93 +28,117 @@ inline RowShape row_shape(long long chunks) {
     while (r.log_tpr < 8 && (1 << r.log_tpr) < chunks) ++r.log_tpr;
     return r;
 }
-inline dim3 row_grid(const RowShape& r, int M) {
-    const long long groups = ((long long)M + (kThreads >> r.log_tpr) - 1) / (kThreads >> r.log_tpr);
+inline dim3 row_grid(const RowShape& r, long long M) {
+    const long long groups = (M + (kThreads >> r.log_tpr) - 1) / (kThreads >> r.log_tpr);
     return dim3((unsigned)((r.chunks + (1 << r.log_tpr) - 1) >> r.log_tpr), (unsigned)(groups < 65535 ? groups : 65535));
 }
 
-template <int TYPE, bool VEC>
+// AHEAD: rows a thread requests before it quantises the first.
+template <int TYPE, int AHEAD>
 __global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(MxQuantArgs a, RowShape rs, size_t code_pitch, size_t scale_pitch) {
     const int chunk = (int)(blockIdx.x << rs.log_tpr) + (int)(threadIdx.x & ((1u << rs.log_tpr) - 1));
     if (chunk >= rs.chunks) return;                                  // whole quads: chunks is a multiple of 16
     const int rows = kThreads >> rs.log_tpr, j0 = 8 * chunk, left = a.N - j0;
     typedef typename MxType<TYPE>::value value;
-    for (long long r = (long long)blockIdx.y * rows + (threadIdx.x >> rs.log_tpr); r < a.M; r += (long long)gridDim.y * rows) {
-        const value* src = static_cast<const value*>(a.w) + r * a.ldw + j0;
-        MxEight<TYPE> e;
-        if (VEC && left >= 8) e.load(src);
-        else e.load_some(src, min(max(left, 0), 8));
-        const u32 byte = mx_scale_byte(mx_magnitude<TYPE>(quad_max(e.top())));
-        reinterpret_cast<u32*>(static_cast<char*>(a.codes) + r * code_pitch)[chunk] = e.pack(byte);
-        if ((chunk & 3) == 0) (static_cast<uint8_t*>(a.scales) + r * scale_pitch)[chunk >> 2] = (uint8_t)byte;
+    const long long step = (long long)gridDim.y * rows;
+    for (long long r = (long long)blockIdx.y * rows + (threadIdx.x >> rs.log_tpr); r < a.M; r += AHEAD * step) {
+        MxEight<TYPE> e[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (r + k * step < a.M) e[k].load(static_cast<const value*>(a.w) + (r + k * step) * a.ldw + j0, left, chunk == 0);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (r + k * step >= a.M) break;
+            const u32 byte = mx_scale_byte(mx_magnitude<TYPE>(quad_max(e[k].top())));
+            reinterpret_cast<u32*>(static_cast<char*>(a.codes) + (r + k * step) * code_pitch)[chunk] = e[k].pack(byte);
+            if ((chunk & 3) == 0) (static_cast<uint8_t*>(a.scales) + (r + k * step) * scale_pitch)[chunk >> 2] = (uint8_t)byte;
+        }
     }
 }
 
-template <int TYPE, bool VEC>
+// Sixteen bytes of the result to a thread: eight elements, or four in fp32, so that neighbouring lanes write whole lines with one store.
+template <int TYPE>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxDequantArgs a, RowShape rs, size_t code_pitch, size_t scale_pitch) {
+    constexpr int E = TYPE == SQLLM_F32 ? 4 : 8;
     const int chunk = (int)(blockIdx.x << rs.log_tpr) + (int)(threadIdx.x & ((1u << rs.log_tpr) - 1));
     if (chunk >= rs.chunks) return;
-    const int rows = kThreads >> rs.log_tpr, j0 = 8 * chunk, left = a.N - j0;
+    const int rows = kThreads >> rs.log_tpr, j0 = E * chunk, left = a.N - j0;
     typedef typename MxType<TYPE>::value value;
     for (long long r = (long long)blockIdx.y * rows + (threadIdx.x >> rs.log_tpr); r < a.M; r += (long long)gridDim.y * rows) {
-        const u32 codes = reinterpret_cast<const u32*>(static_cast<const char*>(a.codes) + r * code_pitch)[chunk];
-        const u32 byte = (static_cast<const uint8_t*>(a.scales) + r * scale_pitch)[chunk >> 2];
-        MxEight<TYPE> e;
-        e.unpack(codes, byte);
+        const char* codes = static_cast<const char*>(a.codes) + r * code_pitch;
+        const u32 byte = (static_cast<const uint8_t*>(a.scales) + r * scale_pitch)[j0 / kMxBlock];
         value* dst = static_cast<value*>(a.w) + r * a.ldw + j0;
-        if (VEC && left >= 8) e.store(dst);
-        else e.store_some(dst, min(left, 8));
+        MxEight<TYPE> e;
+        if constexpr (TYPE == SQLLM_F32) {
+            e.unpack(reinterpret_cast<const uint16_t*>(codes)[chunk], byte);
+            if (left >= 4) __builtin_nontemporal_store(u32x4{e.v[0], e.v[1], e.v[2], e.v[3]}, reinterpret_cast<u32x4_a4*>(dst));
+            else e.store_some(dst, left);
+        } else {
+            e.unpack(reinterpret_cast<const u32*>(codes)[chunk], byte);
+            if (left >= 8) e.store(dst);
+            else e.store_some(dst, left);
+        }
     }
 }
 
 // ---------------------------------------------------------------------------------------------- columns: quantise the transpose
 // A workgroup takes a tile of 128 x 128 elements through LDS: eights of the rows go in as they are loaded (and, where the row direction is
-// asked for too, are quantised on the way, so w is read once for both), then every thread walks down 32 rows of a column.
+// asked for too, are quantised on the way, so w is read once for both), then every thread walks down 32 rows of a column, or of two.  Codes and
+// scales of the columns, and scales of the rows, are gathered in LDS and leave four neighbouring bytes, or sixteen, to a lane: a byte of a row of
+// its own from every lane took longer (5120 x 5120 fp16, both directions: 28.0
+// against 24.8 us; with the loads past the caches 21.8).
 constexpr int kTile = 128;
 
-template <int TYPE, bool VEC, bool ROWS>
-__global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs a, int tiles_n, size_t code_pitch, size_t scale_pitch, size_t code_pitch_t, size_t scale_pitch_t) {
+template <int TYPE, bool ROWS>
+__global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs a, int tiles_m, int tiles_n, size_t code_pitch, size_t scale_pitch, size_t code_pitch_t, size_t scale_pitch_t) {
     typedef typename MxType<TYPE>::value value;
     constexpr int D = MxEight<TYPE>::kDwords, kPitch = kTile / 8 * D;   // dwords of a row
     extern __shared__ __align__(16) u32 tile[];
+    __shared__ u32 row_scales[kTile], column_scales[kTile];          // the four scale bytes of a row, of a column
     const int tid = threadIdx.x;
-    const int tm = blockIdx.x / tiles_n, tn = blockIdx.x % tiles_n;
-    const long long m0 = (long long)tm * kTile;
-    const int n0 = tn * kTile, chunk = tid & 15;
+    // the XCDs, to which workgroups are handed in turn, take contiguous ranges of the tiles in bands of eight columns of them: neighbours, whose outputs
+    // share cache lines, write through the same L2
+    const int tiles = tiles_m * tiles_n, xcd = blockIdx.x & 7;
+    const int p = (int)((long long)tiles * xcd >> 3) + (int)(blockIdx.x >> 3);
+    if (p >= (int)((long long)tiles * (xcd + 1) >> 3)) return;
+    const int band = p / (8 * tiles_m), at = p % (8 * tiles_m), wide = min(tiles_n - 8 * band, 8);
+    const long long m0 = (long long)(at / wide) * kTile;
+    const int n0 = (8 * band + at % wide) * kTile, chunk = tid & 15;
+    MxEight<TYPE> in[kTile / 16];                                    // all of a thread's share on its way before the first is used
 #pragma unroll
     for (int p = 0; p < kTile / 16; ++p) {
         const int row = 16 * p + (tid >> 4), left = m0 + row < a.M ? a.N - (n0 + 8 * chunk) : 0;
-        MxEight<TYPE> e;
-        const value* src = static_cast<const value*>(a.w) + (m0 + row) * a.ldw + n0 + 8 * chunk;
-        if (VEC && left >= 8) e.load(src);
-        else e.load_some(src, min(max(left, 0), 8));
-        e.store(tile + row * kPitch + chunk * D);
+        in[p].load(static_cast<const value*>(a.w) + (m0 + row) * a.ldw + n0 + 8 * chunk, left, n0 + chunk == 0);
+    }
+#pragma unroll
+    for (int p = 0; p < kTile / 16; ++p) {
+        const int row = 16 * p + (tid >> 4);
+        in[p].to_lds(tile + row * kPitch + chunk * D);
         if (ROWS) {
-            const u32 byte = mx_scale_byte(mx_magnitude<TYPE>(quad_max(e.top())));
-            const u32 packed = e.pack(byte);
-            if (m0 + row < a.M) {
-                reinterpret_cast<u32*>(static_cast<char*>(a.codes) + (m0 + row) * code_pitch)[n0 / 8 + chunk] = packed;
-                if ((chunk & 3) == 0) (static_cast<uint8_t*>(a.scales) + (m0 + row) * scale_pitch)[n0 / 32 + (chunk >> 2)] = (uint8_t)byte;
-            }
+            const u32 byte = mx_scale_byte(mx_magnitude<TYPE>(quad_max(in[p].top())));
+            const u32 packed = in[p].pack(byte);
+            if (m0 + row < a.M) reinterpret_cast<u32*>(static_cast<char*>(a.codes) + (m0 + row) * code_pitch)[n0 / 8 + chunk] = packed;
+            if ((chunk & 3) == 0) reinterpret_cast<uint8_t*>(row_scales)[4 * row + (chunk >> 2)] = (uint8_t)byte;
         }
     }
     __syncthreads();
-    auto put = [&](int col, int b, const MxEight<TYPE> (&e)[4]) {     // block b of the tile's column
+    u32x4 out[2];                                                    // codes of block b of two columns
+    int column[2], block[2];
+    auto take = [&](int k, int col, int b, const MxEight<TYPE> (&e)[4]) {
         const u32 byte = mx_scale_byte(mx_magnitude<TYPE>(max(max(e[0].top(), e[1].top()), max(e[2].top(), e[3].top()))));
-        if (n0 + col < a.N) {
-            *reinterpret_cast<u32x4*>(static_cast<char*>(a.codes_t) + (size_t)(n0 + col) * code_pitch_t + m0 / 2 + 16 * b) =
-                u32x4{e[0].pack(byte), e[1].pack(byte), e[2].pack(byte), e[3].pack(byte)};
-            (static_cast<uint8_t*>(a.scales_t) + (size_t)(n0 + col) * scale_pitch_t)[m0 / 32 + b] = (uint8_t)byte;
-        }
+        out[k] = u32x4{e[0].pack(byte), e[1].pack(byte), e[2].pack(byte), e[3].pack(byte)};
+        column[k] = col; block[k] = b;
+        reinterpret_cast<uint8_t*>(column_scales)[4 * col + b] = (uint8_t)byte;
     };
     if constexpr (TYPE == SQLLM_F32) {
         const int col = tid & 127;
 #pragma unroll
-        for (int b = tid >> 7; b < 4; b += 2) {
+        for (int k = 0; k < 2; ++k) {
+            const int b = (tid >> 7) + 2 * k;
             MxEight<TYPE> e[4];
 #pragma unroll
-            for (int k = 0; k < 32; ++k) e[k >> 3].v[k & 7] = tile[(32 * b + k) * kPitch + col];
-            put(col, b, e);
+            for (int i = 0; i < 32; ++i) e[i >> 3].v[i & 7] = tile[(32 * b + i) * kPitch + col];
+            take(k, col, b, e);
         }
     } else {
         const int b = tid >> 6, pair = tid & 63;                     // two neighbouring columns
@@ -125,8 +149,25 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs 
             lo[k >> 3].v[(k & 7) >> 1] = __builtin_amdgcn_perm(r1, r0, 0x05040100u);
             hi[k >> 3].v[(k & 7) >> 1] = __builtin_amdgcn_perm(r1, r0, 0x07060302u);
         }
-        put(2 * pair, b, lo);
-        put(2 * pair + 1, b, hi);
+        take(0, 2 * pair, b, lo);
+        take(1, 2 * pair + 1, b, hi);
+    }
+    __syncthreads();                                                 // the tile is read: its place takes the codes of the columns, 64 bytes each
+    // block b of column c at position b ^ (c / 2): neighbouring lanes write and read different banks
+#pragma unroll
+    for (int k = 0; k < 2; ++k) *reinterpret_cast<u32x4*>(tile + 16 * column[k] + 4 * (block[k] ^ ((column[k] >> 1) & 3))) = out[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int col = (tid >> 2) + 64 * k, b = tid & 3;
+        if (n0 + col < a.N)
+            *reinterpret_cast<u32x4*>(static_cast<char*>(a.codes_t) + (size_t)(n0 + col) * code_pitch_t + m0 / 2 + 16 * b) = *reinterpret_cast<const u32x4*>(tile + 16 * col + 4 * (b ^ ((col >> 1) & 3)));
+    }
+    if (tid < kTile) {
+        if (n0 + tid < a.N) *reinterpret_cast<u32*>(static_cast<char*>(a.scales_t) + (size_t)(n0 + tid) * scale_pitch_t + m0 / 32) = column_scales[tid];
+    } else if (ROWS) {
+        const int row = tid - kTile;
+        if (m0 + row < a.M) *reinterpret_cast<u32*>(static_cast<char*>(a.scales) + (m0 + row) * scale_pitch + n0 / 32) = row_scales[row];
     }
 }
 
@@ -438,35 +479,37 @@ __global__ void __launch_bounds__(kBatchWaves * 64, 2) mx_gemv_batch_kernel(MxGe
 // ---------------------------------------------------------------------------------------------- launchers
 namespace {
 
-bool vector_rows(const void* p, long long ld, int size) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0; }
-
 template <int TYPE>
 hipError_t quantize(const MxQuantArgs& a, hipStream_t s) {
-    const bool vec = vector_rows(a.w, a.ldw, mx_type_size(TYPE));
     const size_t cp = mx_row_code_bytes(a.N), sp = mx_row_scale_bytes(a.N);
     if (a.codes_t) {
         const int tiles_n = mx_padded(a.N) / kTile, tiles_m = mx_padded(a.M) / kTile;
         const size_t cpt = mx_row_code_bytes(a.M), spt = mx_row_scale_bytes(a.M);
         const unsigned lds = kTile * (kTile / 8) * MxEight<TYPE>::kDwords * 4;
-        const dim3 grid((unsigned)((long long)tiles_m * tiles_n));
-        if (vec && a.codes) mx_quantize_tile_kernel<TYPE, true, true><<<grid, kThreads, lds, s>>>(a, tiles_n, cp, sp, cpt, spt);
-        else if (vec) mx_quantize_tile_kernel<TYPE, true, false><<<grid, kThreads, lds, s>>>(a, tiles_n, cp, sp, cpt, spt);
-        else if (a.codes) mx_quantize_tile_kernel<TYPE, false, true><<<grid, kThreads, lds, s>>>(a, tiles_n, cp, sp, cpt, spt);
-        else mx_quantize_tile_kernel<TYPE, false, false><<<grid, kThreads, lds, s>>>(a, tiles_n, cp, sp, cpt, spt);
+        const dim3 grid((unsigned)(((long long)tiles_m * tiles_n + 7) / 8 * 8));
+        if (lds > 65536 - 2048) {                                    // with the scales above what a launch gets without asking
+            const hipError_t e = hipFuncSetAttribute(a.codes ? reinterpret_cast<const void*>(&mx_quantize_tile_kernel<TYPE, true>) : reinterpret_cast<const void*>(&mx_quantize_tile_kernel<TYPE, false>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return e;
+        }
+        if (a.codes) mx_quantize_tile_kernel<TYPE, true><<<grid, kThreads, lds, s>>>(a, tiles_m, tiles_n, cp, sp, cpt, spt);
+        else mx_quantize_tile_kernel<TYPE, false><<<grid, kThreads, lds, s>>>(a, tiles_m, tiles_n, cp, sp, cpt, spt);
     } else {
+        // Four rows ahead where that leaves eight workgroups to a compute unit: 11008 x 4096 fp16 25.2 -> 21.8 us, but 301 x 5120 3.2 -> 3.7.  Not in fp32, where a
+        // row is two loads already: 40 -> 43 us.
         const RowShape rs = row_shape(mx_padded(a.N) / 8);
-        if (vec) mx_quantize_rows_kernel<TYPE, true><<<row_grid(rs, a.M), kThreads, 0, s>>>(a, rs, cp, sp);
-        else mx_quantize_rows_kernel<TYPE, false><<<row_grid(rs, a.M), kThreads, 0, s>>>(a, rs, cp, sp);
+        const dim3 few = row_grid(rs, (a.M + 3ll) / 4);
+        if (TYPE != SQLLM_F32 && (long long)few.x * few.y >= 2048) mx_quantize_rows_kernel<TYPE, 4><<<few, kThreads, 0, s>>>(a, rs, cp, sp);
+        else mx_quantize_rows_kernel<TYPE, 1><<<row_grid(rs, a.M), kThreads, 0, s>>>(a, rs, cp, sp);
     }
     return hipGetLastError();
 }
 
 template <int TYPE>
 hipError_t dequantize(const MxDequantArgs& a, hipStream_t s) {
-    const RowShape rs = row_shape(((long long)a.N + 7) / 8);
-    const size_t cp = mx_row_code_bytes(a.N), sp = mx_row_scale_bytes(a.N);
-    if (vector_rows(a.w, a.ldw, mx_type_size(TYPE))) mx_dequantize_kernel<TYPE, true><<<row_grid(rs, a.M), kThreads, 0, s>>>(a, rs, cp, sp);
-    else mx_dequantize_kernel<TYPE, false><<<row_grid(rs, a.M), kThreads, 0, s>>>(a, rs, cp, sp);
+    constexpr int E = TYPE == SQLLM_F32 ? 4 : 8;
+    const RowShape rs = row_shape(((long long)a.N + E - 1) / E);
+    mx_dequantize_kernel<TYPE><<<row_grid(rs, a.M), kThreads, 0, s>>>(a, rs, mx_row_code_bytes(a.N), mx_row_scale_bytes(a.N));
     return hipGetLastError();
 }
 

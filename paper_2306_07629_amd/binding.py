@@ -1,4 +1,4 @@
-"""ctypes binding of the C ABI in include/sqllm.h (the matvec call also natively, csrc/sqllm_pycall.c).  Argument marshalling
+"""ctypes binding of the C ABI in include/sqllm.h (the matvec call and the sqllm_mx_* calls also natively, csrc/sqllm_pycall.c).  Argument marshalling
 only: every step of the matvec runs in the HIP kernels of libsqllm.so.  PyTorch tensors are used as owners of device memory and for the
 current HIP stream, nothing else.  There is no CPU fallback: a missing library raises."""
 from __future__ import annotations
@@ -122,9 +122,15 @@ def _matvec_ctypes(M, N, bits, nnz, B, qidx, lut, rowptr, cols, vals, plan, x, y
                                            _ptr(x), _ptr(y), _stream(stream))
 
 
-def _native_matvec():
-    """The native form of the call; None where its module cannot be built or imported (said once): ctypes does the same."""
-    address = ctypes.cast(lib().sqllm_dense_sparse_matvec, ctypes.c_void_p).value
+_MX_ENTRIES = ("sqllm_mx_quantize", "sqllm_mx_dequantize", "sqllm_mx_gemv", "sqllm_mx_gemm")   # by their number in csrc/sqllm_pycall.c
+
+
+def _address(fn):
+    return ctypes.cast(fn, ctypes.c_void_p).value
+
+
+def _native_module():
+    """The native form of the calls; None where its module cannot be built or imported (said once): ctypes does the same."""
     try:
         if _build.pycall_is_stale():
             _build.build_pycall()
@@ -134,8 +140,16 @@ def _native_matvec():
         return None
     if _torch is None:
         _find_streams()
-    _pycall.bind(address, _torch.cuda.current_device, _raw_stream)
-    return _pycall.matvec
+    L = lib()
+    _pycall.bind(_address(L.sqllm_dense_sparse_matvec), _torch.cuda.current_device, _raw_stream)
+    _pycall.bind_mx(*[_address(getattr(L, name)) for name in _MX_ENTRIES], _torch.cuda.current_device, _raw_stream)
+    return _pycall
+
+
+def _native_matvec():
+    lib()
+    module = _native_module()
+    return module and module.matvec
 
 
 def _matvec_first(*args):
@@ -237,20 +251,44 @@ def sqllm_mx_bytes(M, N):
     return int(c.value), int(s.value)
 
 
+def _mx_ctypes(entry, *args):
+    *rest, stream = args
+    return getattr(lib(), _MX_ENTRIES[entry])(*[t.data_ptr() if hasattr(t, "data_ptr") else t for t in rest], _stream(stream))
+
+
+def _mx_first(*args):
+    """The first call chooses the path of all later ones."""
+    global _mx_call
+    module = _native_module()
+    _mx_call = module.mx if module else _mx_ctypes
+    return _mx_call(*args)
+
+
+_mx_call = _mx_first
+
+
+def _mx(*args):
+    status = _mx_call(*args)
+    if status is None:                                                # arguments that only ctypes knows how to take, or to refuse
+        status = _mx_ctypes(*args)
+    if status:
+        _check(status)
+
+
 def sqllm_mx_quantize(M, N, type, w, ldw, codes, scales, codes_t=None, scales_t=None, stream=None):
-    _check(lib().sqllm_mx_quantize(M, N, type, _ptr(w), ldw, _ptr(codes), _ptr(scales), _ptr(codes_t), _ptr(scales_t), _stream(stream)))
+    _mx(0, M, N, type, w, ldw, codes, scales, codes_t, scales_t, stream)
 
 
 def sqllm_mx_dequantize(M, N, type, codes, scales, w_out, ldw, stream=None):
-    _check(lib().sqllm_mx_dequantize(M, N, type, _ptr(codes), _ptr(scales), _ptr(w_out), ldw, _stream(stream)))
+    _mx(1, M, N, type, codes, scales, w_out, ldw, stream)
 
 
 def sqllm_mx_gemv(M, N, B, codes, scales, x, y, accumulate=0, stream=None):
-    _check(lib().sqllm_mx_gemv(M, N, B, _ptr(codes), _ptr(scales), _ptr(x), _ptr(y), int(accumulate), _stream(stream)))
+    _mx(2, M, N, B, codes, scales, x, y, int(accumulate), stream)
 
 
 def sqllm_mx_gemm(T, M, N, type, x_codes, x_scales, w_codes, w_scales, y, ldy, accumulate=0, stream=None):
-    _check(lib().sqllm_mx_gemm(T, M, N, type, _ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(y), ldy, int(accumulate), _stream(stream)))
+    _mx(3, T, M, N, type, x_codes, x_scales, w_codes, w_scales, y, ldy, int(accumulate), stream)
 
 
 def sqllm_version() -> int:

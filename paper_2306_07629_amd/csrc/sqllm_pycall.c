@@ -1,9 +1,10 @@
-/* One call of sqllm_dense_sparse_matvec from Python without ctypes: takes the arguments apart, asks the tensors for their addresses and the
+/* One call of sqllm_dense_sparse_matvec, or of one of the sqllm_mx_* entry points, from Python without ctypes: takes the arguments apart, asks the tensors for their addresses and the
  * runtime for the current stream, and calls the library.  The call of a small layer is bound by the host: through ctypes 256x4096 takes
  * 5.6 us and 4096x4096 at 4 bits 5.8, this way 4.5 and 4.5 (their kernels run for 3.0 and 4.4).  Arguments that are not plain ints, None or
  * objects with data_ptr() are left to the ctypes path (None is returned), which accepts or refuses them as it always has. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <string.h>
 
 typedef int (*matvec_fn)(int, int, int, long long, int, const void*, const void*, const int*, const int*, const void*, const void*, const void*, void*, void*);
 
@@ -39,6 +40,21 @@ static int address_of(PyObject* o, PyObject* method, int call, void** out) {
     return PyErr_Occurred() ? -1 : 1;
 }
 
+/* handle of a stream, None: the current one of the current device; returns as address_of */
+static int stream_of(PyObject* o, PyObject* device, PyObject* stream, void** out) {
+    PyObject *dev, *s;
+    int st;
+    if (o != Py_None) return address_of(o, s_cuda_stream, 0, out);
+    dev = PyObject_CallNoArgs(device);
+    if (!dev) return -1;
+    s = PyObject_CallOneArg(stream, dev);
+    Py_DECREF(dev);
+    if (!s) return -1;
+    st = PyLong_Check(s) ? address_of(s, NULL, 0, out) : 0;
+    Py_DECREF(s);
+    return st;
+}
+
 /* matvec(M, N, bits, nnz, B, qidx, lut, rowptr, cols, vals, plan, x, y, stream) -> status, or None */
 static PyObject* matvec(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     long long v[5];
@@ -56,17 +72,7 @@ static PyObject* matvec(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         if (st < 0) return NULL;
         if (st == 0) Py_RETURN_NONE;
     }
-    if (a[13] == Py_None) {
-        PyObject *dev = PyObject_CallNoArgs(g_device), *s;
-        if (!dev) return NULL;
-        s = PyObject_CallOneArg(g_stream, dev);
-        Py_DECREF(dev);
-        if (!s) return NULL;
-        st = PyLong_Check(s) ? address_of(s, NULL, 0, &p[8]) : 0;
-        Py_DECREF(s);
-    } else {
-        st = address_of(a[13], s_cuda_stream, 0, &p[8]);
-    }
+    st = stream_of(a[13], g_device, g_stream, &p[8]);
     if (st < 0) return NULL;
     if (st == 0) Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS
@@ -75,7 +81,72 @@ static PyObject* matvec(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
+/* The sqllm_mx_* entry points: i an int, l a long long, p a pointer, s the stream. */
+enum { kQuantize, kDequantize, kGemv, kGemm, kEntries };
+static const char* const g_kinds[kEntries] = {"iiiplpppps", "iiipppls", "iiippppis", "iiiippppplis"};
+static void* g_mx[kEntries];
+static PyObject *g_mx_device, *g_mx_stream;      /* as g_device and g_stream */
+typedef int (*quantize_fn)(int, int, int, const void*, long long, void*, void*, void*, void*, void*);
+typedef int (*dequantize_fn)(int, int, int, const void*, const void*, void*, long long, void*);
+typedef int (*gemv_fn)(int, int, int, const void*, const void*, const void*, void*, int, void*);
+typedef int (*gemm_fn)(int, int, int, int, const void*, const void*, const void*, const void*, void*, long long, int, void*);
+
+static PyObject* bind_mx(PyObject* self, PyObject* args) {
+    unsigned long long a[kEntries];
+    PyObject *device, *stream;
+    int i;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "KKKKOO", &a[0], &a[1], &a[2], &a[3], &device, &stream)) return NULL;
+    Py_INCREF(device);
+    Py_INCREF(stream);
+    Py_XSETREF(g_mx_device, device);
+    Py_XSETREF(g_mx_stream, stream);
+    for (i = 0; i < kEntries; ++i) g_mx[i] = (void*)(uintptr_t)a[i];
+    Py_RETURN_NONE;
+}
+
+/* mx(entry, its arguments...) -> status, or None */
+static PyObject* mx(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    long long v[12];                                                  /* integers and pointers by position */
+    void* p[12];
+    long entry;
+    const char* kinds;
+    int i, st;
+    (void)self;
+    if (n < 1 || !PyLong_Check(a[0])) Py_RETURN_NONE;
+    entry = PyLong_AsLong(a[0]);
+    if (entry < 0 || entry >= kEntries) {
+        if (PyErr_Occurred()) return NULL;
+        Py_RETURN_NONE;
+    }
+    kinds = g_kinds[entry];
+    if (!g_mx[entry] || n != 1 + (Py_ssize_t)strlen(kinds)) Py_RETURN_NONE;
+    for (i = 0; kinds[i]; ++i) {
+        PyObject* o = a[1 + i];
+        if (kinds[i] == 'i' || kinds[i] == 'l') {
+            if (!PyLong_Check(o)) Py_RETURN_NONE;
+            v[i] = (long long)PyLong_AsUnsignedLongLongMask(o);
+            if (PyErr_Occurred()) return NULL;
+            continue;
+        }
+        st = kinds[i] == 's' ? stream_of(o, g_mx_device, g_mx_stream, &p[i]) : address_of(o, s_data_ptr, 1, &p[i]);
+        if (st < 0) return NULL;
+        if (st == 0) Py_RETURN_NONE;
+    }
+    Py_BEGIN_ALLOW_THREADS
+    switch (entry) {
+        case kQuantize: st = ((quantize_fn)g_mx[entry])((int)v[0], (int)v[1], (int)v[2], p[3], v[4], p[5], p[6], p[7], p[8], p[9]); break;
+        case kDequantize: st = ((dequantize_fn)g_mx[entry])((int)v[0], (int)v[1], (int)v[2], p[3], p[4], p[5], v[6], p[7]); break;
+        case kGemv: st = ((gemv_fn)g_mx[entry])((int)v[0], (int)v[1], (int)v[2], p[3], p[4], p[5], p[6], (int)v[7], p[8]); break;
+        default: st = ((gemm_fn)g_mx[entry])((int)v[0], (int)v[1], (int)v[2], (int)v[3], p[4], p[5], p[6], p[7], p[8], v[9], (int)v[10], p[11]); break;
+    }
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
 static PyMethodDef methods[] = {
+    {"bind_mx", bind_mx, METH_VARARGS, NULL},
+    {"mx", (PyCFunction)(void (*)(void))mx, METH_FASTCALL, NULL},
     {"bind", bind, METH_VARARGS, NULL},
     {"matvec", (PyCFunction)(void (*)(void))matvec, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},

@@ -2,8 +2,6 @@
 arguments (no arithmetic here); every call enqueues on the current stream of its tensors' device."""
 from __future__ import annotations
 
-import contextlib
-
 import torch
 
 from . import binding
@@ -16,9 +14,16 @@ def _refuse(name, message):
     raise binding.SqllmError(binding.STATUS_NAMES.index(name), message)
 
 
-def _on(device):
-    """the device of the tensors as the current one"""
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+def _call(device, fn, *args):
+    """fn(*args) with the device of the tensors as the current one"""
+    if device == _current_device():
+        fn(*args)
+    else:
+        with torch.cuda.device(device):
+            fn(*args)
+
+
+_current_device = torch.cuda.current_device
 
 
 def _type_of(dtype):
@@ -27,21 +32,24 @@ def _type_of(dtype):
     return _TYPES[dtype]
 
 
-def _need(t, what, device=None, dtype=None, shape=None):
+def _need(t, what, like=None, dtype=None, shape=None):
+    """t is on a GPU (that of `like`), of that type and shape"""
     if not t.is_cuda:
         _refuse("SQLLM_ERR_DEVICE", f"{what} is not on a GPU")
-    if device is not None and t.device != device:
-        _refuse("SQLLM_ERR_DEVICE", f"{what} is on {t.device}, not on {device}")
-    if dtype is not None and t.dtype != dtype:
+    if like is not None and t.get_device() != like.get_device():
+        _refuse("SQLLM_ERR_DEVICE", f"{what} is on {t.device}, not on {like.device}")
+    if dtype is not None and t.dtype is not dtype:
         _refuse("SQLLM_ERR_TYPE", f"{what} is {t.dtype}, not {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _refuse("SQLLM_ERR_SHAPE", f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
+    if shape is not None and t.shape != shape:
+        _refuse("SQLLM_ERR_SHAPE", f"{what} is {tuple(t.shape)}, not {shape}")
 
 
 def _rows(t, what):
     """a matrix the library can walk by rows, and its row stride: t itself or a contiguous copy"""
     if t.dim() != 2:
         _refuse("SQLLM_ERR_SHAPE", f"{what} has {t.dim()} dimensions, not 2")
+    if t.is_contiguous():
+        return t, t.shape[1]
     if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
         t = t.contiguous()
     return t, (t.stride(0) if t.shape[0] > 1 else t.shape[1])
@@ -57,15 +65,21 @@ class MxMatrix:
             _refuse("SQLLM_ERR_SHAPE", f"a packed matrix of {M} x {N}")
         padded = -(-N // ROW) * ROW
         for t, what, width in ((codes, "codes", padded // 2), (scales, "scales", padded // 32)):
-            _need(t, what, codes.device, torch.uint8, (M, width))
+            _need(t, what, codes, torch.uint8, (M, width))
             if not t.is_contiguous():
                 _refuse("SQLLM_ERR_SHAPE", f"{what} are not contiguous")
         self.M, self.N, self.codes, self.scales = M, N, codes, scales
 
     @staticmethod
     def empty(M, N, device):
+        if M < 0 or N <= 0:
+            _refuse("SQLLM_ERR_SHAPE", f"a packed matrix of {M} x {N}")
         padded = -(-N // ROW) * ROW
-        return MxMatrix(M, N, torch.empty((M, padded // 2), dtype=torch.uint8, device=device), torch.empty((M, padded // 32), dtype=torch.uint8, device=device))
+        m = object.__new__(MxMatrix)
+        m.M, m.N = M, N
+        m.codes = torch.empty((M, padded // 2), dtype=torch.uint8, device=device)
+        m.scales = torch.empty((M, padded // 32), dtype=torch.uint8, device=device)
+        return m
 
     @property
     def device(self):
@@ -74,9 +88,9 @@ class MxMatrix:
     def dequantize(self, dtype=torch.float16) -> torch.Tensor:
         """the numbers it holds, [M, N]"""
         ty = _type_of(dtype)
-        out = torch.empty((self.M, self.N), dtype=dtype, device=self.device)
-        with _on(self.device):
-            binding.sqllm_mx_dequantize(self.M, self.N, ty, self.codes, self.scales, out, self.N)
+        codes = self.codes
+        out = torch.empty((self.M, self.N), dtype=dtype, device=codes.device)
+        _call(codes.get_device(), binding.sqllm_mx_dequantize, self.M, self.N, ty, codes, self.scales, out, self.N)
         return out
 
 
@@ -89,27 +103,26 @@ def mx_quantize(w: torch.Tensor, direction: str = "rows"):
     ty = _type_of(w.dtype)
     w, ld = _rows(w, "w")
     M, N = w.shape
-    with _on(w.device):
-        rows = MxMatrix.empty(M, N, w.device) if direction != "columns" else None
-        columns = MxMatrix.empty(N, M, w.device) if direction != "rows" else None
-        binding.sqllm_mx_quantize(M, N, ty, w, ld, rows and rows.codes, rows and rows.scales, columns and columns.codes, columns and columns.scales)
+    device = w.device
+    rows = MxMatrix.empty(M, N, device) if direction != "columns" else None
+    columns = MxMatrix.empty(N, M, device) if direction != "rows" else None
+    _call(w.get_device(), binding.sqllm_mx_quantize, M, N, ty, w, ld, rows and rows.codes, rows and rows.scales, columns and columns.codes, columns and columns.scales)
     return (rows, columns) if direction == "both" else rows or columns
 
 
 def mx_gemv(w: MxMatrix, x: torch.Tensor, y: torch.Tensor | None = None, accumulate: bool = False) -> torch.Tensor:
     """W x for fp16 x [N, B], B = 1..16, as fp16 [M, B]; with accumulate, y + W x in y"""
-    B = x.shape[1] if x.dim() == 2 else 0
-    _need(x, "x", w.device, torch.float16, (w.N, B))
+    codes, B = w.codes, x.shape[1] if x.dim() == 2 else 0
+    _need(x, "x", codes, torch.float16, (w.N, B))
     if y is None:
         if accumulate:
             _refuse("SQLLM_ERR_NULL", "accumulate needs y")
-        y = torch.empty((w.M, B), dtype=torch.float16, device=w.device)
+        y = torch.empty((w.M, B), dtype=torch.float16, device=codes.device)
     else:
-        _need(y, "y", w.device, torch.float16, (w.M, B))
+        _need(y, "y", codes, torch.float16, (w.M, B))
         if not y.is_contiguous():
             _refuse("SQLLM_ERR_SHAPE", "y is not contiguous")
-    with _on(w.device):
-        binding.sqllm_mx_gemv(w.M, w.N, B, w.codes, w.scales, x.contiguous(), y, accumulate)
+    _call(codes.get_device(), binding.sqllm_mx_gemv, w.M, w.N, B, codes, w.scales, x.contiguous(), y, accumulate)
     return y
 
 
@@ -117,22 +130,22 @@ def mx_gemm(x: MxMatrix, w: MxMatrix, dtype=torch.float16, y: torch.Tensor | Non
     """x w^T of two packed matrices with the same number of columns, [x.M, w.M]; y: where to (its type then counts), with accumulate added to what it holds"""
     if x.N != w.N:
         _refuse("SQLLM_ERR_SHAPE", f"x has {x.N} columns, w has {w.N}")
-    if x.device != w.device:
+    codes = w.codes
+    if x.codes.get_device() != codes.get_device():
         _refuse("SQLLM_ERR_DEVICE", f"x is on {x.device}, w on {w.device}")
     if y is None:
         if accumulate:
             _refuse("SQLLM_ERR_NULL", "accumulate needs y")
         ty = _type_of(dtype)
-        y = torch.empty((x.M, w.M), dtype=dtype, device=w.device)
+        y = torch.empty((x.M, w.M), dtype=dtype, device=codes.device)
         ld = w.M
     else:
-        _need(y, "y", w.device, None, (x.M, w.M))
+        _need(y, "y", codes, None, (x.M, w.M))
         ty = _type_of(y.dtype)
         ld = y.stride(0) if x.M > 1 else w.M
         if w.M > 1 and y.stride(1) != 1 or ld < w.M:
             _refuse("SQLLM_ERR_SHAPE", f"y has strides {y.stride()}: its rows must be contiguous and must not overlap")
-    with _on(w.device):
-        binding.sqllm_mx_gemm(x.M, w.M, w.N, ty, x.codes, x.scales, w.codes, w.scales, y, ld, accumulate)
+    _call(codes.get_device(), binding.sqllm_mx_gemm, x.M, w.M, w.N, ty, x.codes, x.scales, codes, w.scales, y, ld, accumulate)
     return y
 
 
@@ -145,7 +158,7 @@ def mx_linear_backward(dy: torch.Tensor, x_t: MxMatrix, w_t: MxMatrix, dtype=Non
     """Gradients of y = Q(x) Q(w)^T (rounding passes gradients through) for dy [T, M]: dx = Q(dy) Q(w) in dtype (that of dy if None), and dw = Q(dy)^T Q(x)
     in fp32, added to `dw` where that is given.  x_t and w_t are the packed transposes of x [T, N] and w [M, N]: mx_quantize(..., "both")[1].
     The blocks of dy lie along the rows for dx and along the columns for dw, as the sums run."""
-    _need(dy, "dy", w_t.device, None, (x_t.N, w_t.N))
+    _need(dy, "dy", w_t.codes, None, (x_t.N, w_t.N))
     rows, columns = mx_quantize(dy, "both")
     dx = mx_gemm(rows, w_t, dy.dtype if dtype is None else dtype)
     if dw is None:

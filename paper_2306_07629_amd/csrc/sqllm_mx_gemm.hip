@@ -135,8 +135,6 @@ __global__ void __launch_bounds__(kFewMaxWaves * 64, 2) mx_gemm_few_kernel(MxGem
 // instructions from the other; one barrier a stage.  Operands are read a step (64 columns) ahead.  Scales go the same way in groups of 512 columns.  Chunk c
 // (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor 16 neighbouring lanes, which read the same chunk of different
 // rows, meet in a bank.
-constexpr int kTileMinColumns = 512;                                 // a group of scales
-
 template <int F>
 struct TileShape {
     static constexpr int kRows = 64 * F;                             // of W and of X
@@ -171,29 +169,29 @@ __device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds,
         const int row0 = R / 8 * wave + lane / kLanes, col = E * (lane % kLanes);
         auto rows = [&](auto add) {                                  // a loop for each: one that does both loses the kind of its stores
 #pragma unroll 4
-        for (int i = 0; i < R / 8; i += 64 / kLanes) {
-            const int row = row0 + i;
-            if (t0 + row >= g.T) continue;
-            vec* y = reinterpret_cast<vec*>(static_cast<value*>(g.y) + (t0 + row) * g.ldy + m0 + col);
-            const float* s = reinterpret_cast<const float*>(lds + row * pitch) + col;
-            float v[E];
+            for (int i = 0; i < R / 8; i += 64 / kLanes) {
+                const int row = row0 + i;
+                if (t0 + row >= g.T) continue;
+                vec* y = reinterpret_cast<vec*>(static_cast<value*>(g.y) + (t0 + row) * g.ldy + m0 + col);
+                const float* s = reinterpret_cast<const float*>(lds + row * pitch) + col;
+                float v[E];
 #pragma unroll
-            for (int k = 0; k < E; k += 4) {
-                const f32x4 t = *reinterpret_cast<const f32x4*>(s + k);
-                v[k] = t.x; v[k + 1] = t.y; v[k + 2] = t.z; v[k + 3] = t.w;
+                for (int k = 0; k < E; k += 4) {
+                    const f32x4 t = *reinterpret_cast<const f32x4*>(s + k);
+                    v[k] = t.x; v[k + 1] = t.y; v[k + 2] = t.z; v[k + 3] = t.w;
+                }
+                vec out;
+                if constexpr (decltype(add)::value) {
+                    const vec old = *y;
+#pragma unroll
+                    for (int k = 0; k < E; ++k) out[k] = (value)((float)old[k] + v[k]);
+                    *y = out;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < E; ++k) out[k] = (value)v[k];
+                    __builtin_nontemporal_store(out, y);                 // 100 -> 84 us for 4096 x 16384 results of 1024 columns
+                }
             }
-            vec out;
-            if constexpr (decltype(add)::value) {
-                const vec old = *y;
-#pragma unroll
-                for (int k = 0; k < E; ++k) out[k] = (value)((float)old[k] + v[k]);
-                *y = out;
-            } else {
-#pragma unroll
-                for (int k = 0; k < E; ++k) out[k] = (value)v[k];
-                __builtin_nontemporal_store(out, y);                 // 100 -> 84 us for 4096 x 16384 results of 1024 columns
-            }
-        }
         };
         if (g.accumulate) rows(std::true_type{});
         else rows(std::false_type{});
@@ -210,7 +208,9 @@ __device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds,
     }
 }
 
-template <int TYPE, int F, bool VEC>
+// SHORT: fewer than 512 columns, so a group of scales is more than a row holds and is fetched dword by dword (5120 x 5120 results of 384 columns in fp32:
+// 30 us, 58 with the kernel for few rows).
+template <int TYPE, int F, bool VEC, bool SHORT>
 __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGemmArgs g, TileOrder order, int K) {
     typedef TileShape<F> S;
     constexpr int R = S::kRows, kStageBytes = S::kStageBytes, kScaleGroupBytes = S::kScaleGroupBytes, NP = S::kPieces;
@@ -255,7 +255,14 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
     auto put = [&](int st, int i) { *reinterpret_cast<i32x4*>(stage + (st & 1) * kStageBytes + 2048 * (i >> 1) + wr[i & 1]) = pre[i]; };
     auto fetch_scales = [&](int gr) {
 #pragma unroll
-        for (int i = 0; i < F / 2; ++i) spre[i] = *reinterpret_cast<const u32x4_a4*>(scales + (size_t)(soff[i] + 4 * (u32)min(4 * gr, ndw - 4)));
+        for (int i = 0; i < F / 2; ++i) {
+            if constexpr (SHORT) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) spre[i][j] = *reinterpret_cast<const u32*>(scales + (size_t)(soff[i] + 4 * (u32)min(4 * gr + j, ndw - 1)));
+            } else {
+                spre[i] = *reinterpret_cast<const u32x4_a4*>(scales + (size_t)(soff[i] + 4 * (u32)min(4 * gr, ndw - 4)));
+            }
+        }
     };
     auto put_scales = [&](int gr) {
         char* b = scale + (gr & 1) * kScaleGroupBytes + wave * (8 * R);
@@ -264,9 +271,14 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
 #pragma unroll
         for (int i = 0; i < F / 2; ++i) {
             u32x4 v = spre[i];
-            v = u32x4{drop1 ? v.y : v.x, drop1 ? v.z : v.y, drop1 ? v.w : v.z, drop1 ? 0u : v.w};
-            v = u32x4{drop2 ? v.z : v.x, drop2 ? v.w : v.y, drop2 ? 0u : v.z, drop2 ? 0u : v.w};
-            v = u32x4{drop4 ? 0u : v.x, drop4 ? 0u : v.y, drop4 ? 0u : v.z, drop4 ? 0u : v.w};
+            if constexpr (SHORT) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = 4 * gr + j < ndw ? v[j] : 0u;
+            } else {
+                v = u32x4{drop1 ? v.y : v.x, drop1 ? v.z : v.y, drop1 ? v.w : v.z, drop1 ? 0u : v.w};
+                v = u32x4{drop2 ? v.z : v.x, drop2 ? v.w : v.y, drop2 ? 0u : v.z, drop2 ? 0u : v.w};
+                v = u32x4{drop4 ? 0u : v.x, drop4 ? 0u : v.y, drop4 ? 0u : v.z, drop4 ? 0u : v.w};
+            }
             const u32 row = 64 * i + lane;
 #pragma unroll
             for (int j = 0; j < 4; ++j) *reinterpret_cast<u32*>(b + 16 * row + 4 * ((j ^ (row >> 3)) & 3)) = v[j];
@@ -409,14 +421,14 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
 
 namespace {
 
-template <int TYPE, int F>
+template <int TYPE, int F, bool SHORT>
 hipError_t gemm_tiles(const MxGemmArgs& g, int K, hipStream_t s) {
     constexpr int R = TileShape<F>::kRows;
     const TileOrder order = {(int)(((long long)g.M + R - 1) / R), (int)(((long long)g.T + R - 1) / R), R};
     const unsigned grid = F == 4 ? 256 : 512;                        // one workgroup to a compute unit, or two
     const bool vec = (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy * mx_type_size(TYPE) % 16 == 0;
-    if (vec) mx_gemm_tile_kernel<TYPE, F, true><<<grid, 256, 0, s>>>(g, order, K);
-    else mx_gemm_tile_kernel<TYPE, F, false><<<grid, 256, 0, s>>>(g, order, K);
+    if (vec) mx_gemm_tile_kernel<TYPE, F, true, SHORT><<<grid, 256, 0, s>>>(g, order, K);
+    else mx_gemm_tile_kernel<TYPE, F, false, SHORT><<<grid, 256, 0, s>>>(g, order, K);
     return hipGetLastError();
 }
 
@@ -433,20 +445,29 @@ hipError_t gemm_few(const MxGemmArgs& g, int K, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Which kernel: the one whose estimate is lowest.  An estimate is a fixed part and a part per 1024 columns (k) for each round of tiles over the compute units,
-// fitted to measured times: 4096 x 16384 results of 1024 / 8192 columns take 81 / 326 us with tiles of 256 and 79 / 375 with 128, 2047 x 4096 of
-// 11008 83 and 67, 301 x 5120 of 5120 42 and 17 (22 with few rows), 128 x 4096 of 11008 29 with 128 and 15 with few rows, 33 x 11008 of 4096 13.4 and 12.
+// Which kernel: the one whose estimate is lowest.  An estimate, in microseconds, is a fixed part and a part per 1024 columns (k) for each round of tiles
+// over the compute units, fitted to measured times: 4096 x 16384 results of 1024 / 8192 columns take 81 / 326 us with tiles of 256 and 79 / 375
+// with 128, 2047 x 4096 of 11008 83 and 67, 301 x 5120 of 5120 42 and 17 (22 with few rows), 128 x 4096 of 11008 29 with 128 and 15 with few rows,
+// 33 x 11008 of 4096 13.4 and 12.
+double cost_of_256(double rows, double others, double k) { return std::ceil(std::ceil(rows / 256) * std::ceil(others / 256) / 256) * (12.6 + 7.6 * k); }
+double cost_of_128(double rows, double others, double k) {
+    const double tiles = std::ceil(rows / 128) * std::ceil(others / 128);
+    return tiles <= 256 ? 4.5 + 2.4 * k : std::ceil(tiles / 512) * (4.2 + 5.2 * k);
+}
+double cost_of_few(double rows, double others, double k) { return 5.8 + (0.0026 + 0.0039 * k) * std::ceil(rows / 32) * std::ceil(others / (others <= 32 ? 32 : 64)); }
+
 template <int TYPE>
 hipError_t gemm(const MxGemmArgs& g, hipStream_t s) {
     const int K = mx_padded(g.N);
-    const double k = K / 1024.0;
-    auto tiles = [&](int m, int t) { return (double)((((long long)g.M + m - 1) / m) * (((long long)g.T + t - 1) / t)); };
-    const double tiles2 = tiles(128, 128);
-    const double cost4 = std::ceil(tiles(256, 256) / 256) * (12.6 + 7.6 * k);
-    const double cost2 = tiles2 <= 256 ? 4.5 + 2.4 * k : std::ceil(tiles2 / 512) * (4.2 + 5.2 * k);
-    const double few = 6.7 + 0.0039 * tiles(32, g.T <= 32 ? 32 : 64) * k;
-    // kTileMinColumns: a group of scales is fetched whole; 2^24: offsets inside a tile are 32 bits
-    if (K >= kTileMinColumns && K <= 1 << 24 && std::min(cost4, cost2) < few) return cost4 < cost2 ? gemm_tiles<TYPE, 4>(g, K, s) : gemm_tiles<TYPE, 2>(g, K, s);
+    const double k = K / 1024.0, cost2 = cost_of_128(g.M, g.T, k), few = cost_of_few(g.M, g.T, k);
+    if (K <= 1 << 24) {                                              // offsets inside a tile are 32 bits
+        if (K < 512) {
+            if (cost2 < few) return gemm_tiles<TYPE, 2, true>(g, K, s);
+        } else {
+            const double cost4 = cost_of_256(g.M, g.T, k);
+            if (std::min(cost4, cost2) < few) return cost4 < cost2 ? gemm_tiles<TYPE, 4, false>(g, K, s) : gemm_tiles<TYPE, 2, false>(g, K, s);
+        }
+    }
     return g.T <= 32 ? gemm_few<TYPE, 1>(g, K, s) : gemm_few<TYPE, 2>(g, K, s);
 }
 

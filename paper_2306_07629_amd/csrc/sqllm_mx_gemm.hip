@@ -132,14 +132,15 @@ __global__ void __launch_bounds__(kFewMaxWaves * 64, 2) mx_gemm_few_kernel(MxGem
 // A workgroup of four waves makes a tile of R rows of W x R rows of X, R = 64 F, each wave a quarter of it in 16 F^2 accumulator registers: F = 4, one wave
 // to a SIMD, or F = 2, two workgroups to a compute unit.  Stages of 256 columns: a wave requests its share of the stage after next into 16 F registers (128
 // bytes of a row to eight lanes, whole cache lines), writes the next stage to the LDS buffer that is not being read, and feeds the matrix
-// instructions from the other; one barrier a stage.  Operands are read a step (64 columns) ahead.  Scales go the same way in groups of 512 columns.  Chunk c
-// (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor 16 neighbouring lanes, which read the same chunk of different
+// instructions from the other; one barrier a stage.  Operands are read a step (64 columns) ahead.  Scales go the same way in groups of 1024 columns, half
+// the rows every second stage: a request is an access of the vector L1 for every row it touches, so two lanes take 32 bytes of a row (in groups of 512, a lane
+// to a row, 2047 x 4096 x 11008 took 74 us, now 69).  Chunk c (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor 16 neighbouring lanes, which read the same chunk of different
 // rows, meet in a bank.
 template <int F>
 struct TileShape {
     static constexpr int kRows = 64 * F;                             // of W and of X
     static constexpr int kStageBytes = 2 * kRows * 128;              // 256 columns of both
-    static constexpr int kScaleGroupBytes = 2 * kRows * 16;          // scales of 512 columns of both
+    static constexpr int kScaleGroupBytes = 2 * kRows * 32;          // scales of 1024 columns of both
     static constexpr int kPieces = 4 * F;                            // 16-byte pieces of a stage per lane
     static constexpr int kPitch = kRows * 4 + 16;                    // of a row of sums in LDS: neighbouring rows four banks apart
     static constexpr int kLds = 2 * kStageBytes + 2 * kScaleGroupBytes;
@@ -208,7 +209,7 @@ __device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds,
     }
 }
 
-// SHORT: fewer than 512 columns, so a group of scales is more than a row holds and is fetched dword by dword (5120 x 5120 results of 384 columns in fp32:
+// SHORT: fewer than 512 columns, so four dwords of scales are more than a row holds and are fetched one by one (5120 x 5120 results of 384 columns in fp32:
 // 30 us, 58 with the kernel for few rows).
 template <int TYPE, int F, bool VEC, bool SHORT>
 __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGemmArgs g, TileOrder order, int K) {
@@ -226,20 +227,19 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
     long long m0, t0;
     order.at(p, m0, t0);
     const u32 cp = K / 2, sp = K / kMxBlock;
-    const int ndw = K / 128, nst = (K + 255) / 256, ngr = (K + 511) / 512;   // dwords of scales of a row, stages, groups of scales
+    const int ndw = K / 128, nst = (K + 255) / 256;   // dwords of scales of a row, stages
     // waves 0, 1 fetch the rows of W, 2, 3 those of X: R / 2 each, eight of them to an instruction; rows past the end repeat the last one
     const bool mine_w = wave < 2;
     const u32 row0 = R / 2 * (wave & 1);
     const char *codes, *scales;
-    u32 off[NP], wr[2], soff[F / 2];
+    u32 off[NP], wr[2];
+    int last;
     auto aim = [&]() {                                               // the fetches at the tile (m0, t0)
         codes = static_cast<const char*>(mine_w ? g.w_codes : g.x_codes) + (size_t)(mine_w ? m0 : t0) * cp;
         scales = static_cast<const char*>(mine_w ? g.w_scales : g.x_scales) + (size_t)(mine_w ? m0 : t0) * sp;
-        const int last = (int)min((mine_w ? (long long)g.M - m0 : (long long)g.T - t0) - 1, (long long)R - 1);
+        last = (int)min((mine_w ? (long long)g.M - m0 : (long long)g.T - t0) - 1, (long long)R - 1);
 #pragma unroll
         for (int i = 0; i < NP; ++i) off[i] = (u32)min((int)(row0 + 8 * i + (lane >> 3)), last) * cp + 16 * (lane & 7);
-#pragma unroll
-        for (int i = 0; i < F / 2; ++i) soff[i] = (u32)min((int)(row0 + 64 * i + lane), last) * sp;
     };
 #pragma unroll
     for (int i = 0; i < 2; ++i) wr[i] = wave * (64 * R) + 128 * (8 * i + (lane >> 3)) + 16 * ((lane & 7) ^ chunk_swizzle(8 * i + (lane >> 3)));
@@ -249,39 +249,45 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
     i32x4 a0[F], b0[F], a1[F], b1[F], pre[NP];
     u32 ua[F], ub[F], va[F], vb[F];
     u32x4 spre[F / 2];
+    const int quad = 4 * (lane & 1);                                 // of a row's eight dwords of a group a lane moves four
     // K is a multiple of 128: the upper half of the last stage may lie behind the rows, and repeats the lower one with scales of 2^-127, whose products
     // vanish against every fp32 number
     auto fetch = [&](int st, int i) { pre[i] = *reinterpret_cast<const i32x4*>(codes + (size_t)min(st, nst - 1) * 128 + off[i] - ((lane & 4) && 2 * min(st, nst - 1) + 1 >= ndw ? 64 : 0)); };
     auto put = [&](int st, int i) { *reinterpret_cast<i32x4*>(stage + (st & 1) * kStageBytes + 2048 * (i >> 1) + wr[i & 1]) = pre[i]; };
-    auto fetch_scales = [&](int gr) {
+    // Part g of the scales: half the rows (g even: the first) of group g / 2.
+    auto fetch_scales = [&](int g) {
+        const int d = 8 * (g >> 1) + quad;
+        int end = last;
+        asm volatile("" : "+s"(end));                                // offsets made anew each time: kept, they would be spilled
 #pragma unroll
         for (int i = 0; i < F / 2; ++i) {
+            const u32 row = __umul24(min((int)(row0 + R / 4 * (g & 1) + 32 * i) + (lane >> 1), end), sp);
             if constexpr (SHORT) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) spre[i][j] = *reinterpret_cast<const u32*>(scales + (size_t)(soff[i] + 4 * (u32)min(4 * gr + j, ndw - 1)));
+                for (int j = 0; j < 4; ++j) spre[i][j] = *reinterpret_cast<const u32*>(scales + (size_t)(row + 4 * (u32)min(d + j, ndw - 1)));
             } else {
-                spre[i] = *reinterpret_cast<const u32x4_a4*>(scales + (size_t)(soff[i] + 4 * (u32)min(4 * gr, ndw - 4)));
+                spre[i] = *reinterpret_cast<const u32x4_a4*>(scales + (size_t)(row + 4 * (u32)min(d, ndw - 4)));
             }
         }
     };
-    auto put_scales = [&](int gr) {
-        char* b = scale + (gr & 1) * kScaleGroupBytes + wave * (8 * R);
-        const int over = max(4 * gr + 4 - ndw, 0);                   // dwords of the group behind the row's end: so much earlier it was fetched
+    auto put_scales = [&](int g) {
+        char* b = scale + ((g >> 1) & 1) * kScaleGroupBytes + wave * (16 * R) + (g & 1) * (8 * R);
+        const int d = 8 * (g >> 1) + quad, over = max(d + 4 - ndw, 0);   // dwords behind the row's end: so much earlier they were fetched
         const bool drop1 = over & 1, drop2 = over & 2, drop4 = over >= 4;
 #pragma unroll
         for (int i = 0; i < F / 2; ++i) {
             u32x4 v = spre[i];
             if constexpr (SHORT) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = 4 * gr + j < ndw ? v[j] : 0u;
+                for (int j = 0; j < 4; ++j) v[j] = d + j < ndw ? v[j] : 0u;
             } else {
                 v = u32x4{drop1 ? v.y : v.x, drop1 ? v.z : v.y, drop1 ? v.w : v.z, drop1 ? 0u : v.w};
                 v = u32x4{drop2 ? v.z : v.x, drop2 ? v.w : v.y, drop2 ? 0u : v.z, drop2 ? 0u : v.w};
                 v = u32x4{drop4 ? 0u : v.x, drop4 ? 0u : v.y, drop4 ? 0u : v.z, drop4 ? 0u : v.w};
             }
-            const u32 row = 64 * i + lane;
+            const u32 row = 32 * i + (lane >> 1);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) *reinterpret_cast<u32*>(b + 16 * row + 4 * ((j ^ (row >> 3)) & 3)) = v[j];
+            for (int j = 0; j < 2; ++j) *reinterpret_cast<u32x2*>(b + 32 * row + 8 * (((quad >> 1) + j) ^ ((row >> 3) & 3))) = u32x2{v[2 * j], v[2 * j + 1]};
         }
     };
     auto read = [&](int st, int s, i32x4 (&a)[F], i32x4 (&b)[F]) {
@@ -293,11 +299,11 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
         }
     };
     auto read_scales = [&](int st) {
-        const char* base = scale + ((st >> 1) & 1) * kScaleGroupBytes + 16 * r + 4 * ((2 * (st & 1) + h) ^ ((r >> 3) & 3));
+        const char* base = scale + ((st >> 2) & 1) * kScaleGroupBytes + 32 * r + 4 * ((2 * (st & 3) + h) ^ (2 * ((r >> 3) & 3)));
 #pragma unroll
         for (int f = 0; f < F; ++f) {
-            va[f] = *reinterpret_cast<const u32*>(base + wm * (8 * R) + 512 * f);
-            vb[f] = *reinterpret_cast<const u32*>(base + 16 * R + wt * (8 * R) + 512 * f);
+            va[f] = *reinterpret_cast<const u32*>(base + wm * (16 * R) + 1024 * f);
+            vb[f] = *reinterpret_cast<const u32*>(base + 32 * R + wt * (16 * R) + 1024 * f);
         }
     };
     auto multiply = [&](auto s, const i32x4 (&a)[F], const i32x4 (&b)[F]) {
@@ -340,8 +346,10 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
         read(st, 3, a1, b1);
 #pragma unroll
         for (int i = 3 * F; i < NP; ++i) { put(st + 1, i); fetch(st + 2, i); }
-        if (kOdd) put_scales((st >> 1) + 1);
-        else fetch_scales((st >> 1) + 1);
+        if (kOdd) {
+            put_scales((st >> 1) + 2);
+            fetch_scales((st >> 1) + 3);
+        }
         multiply(std::integral_constant<int, 2>{}, a0, b0);
 #pragma unroll
         for (int i = 0; i < (F == 4 ? 8 : 2); ++i) {
@@ -365,18 +373,21 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
         __builtin_amdgcn_sched_barrier(0);
     };
     auto request = [&]() {                                           // the first stage and scales of the tile aimed at
-        fetch_scales(0);
 #pragma unroll
         for (int i = 0; i < NP; ++i) fetch(0, i);
+        fetch_scales(0);
     };
     aim();
     request();
     while (true) {
-        put_scales(0);
 #pragma unroll
         for (int i = 0; i < NP; ++i) put(0, i);
+        put_scales(0);
+        fetch_scales(1);
 #pragma unroll
         for (int i = 0; i < NP; ++i) fetch(1, i);
+        put_scales(1);
+        fetch_scales(2);
 #pragma unroll
         for (int i = 0; i < F; ++i)
 #pragma unroll

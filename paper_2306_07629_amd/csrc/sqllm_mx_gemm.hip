@@ -134,8 +134,11 @@ __global__ void __launch_bounds__(kFewMaxWaves * 64, 2) mx_gemm_few_kernel(MxGem
 // bytes of a row to eight lanes, whole cache lines), writes the next stage to the LDS buffer that is not being read, and feeds the matrix
 // instructions from the other; one barrier a stage.  Operands are read a step (64 columns) ahead.  Scales go the same way in groups of 1024 columns, half
 // the rows every second stage: a request is an access of the vector L1 for every row it touches, so two lanes take 32 bytes of a row (in groups of 512, a lane
-// to a row, 2047 x 4096 x 11008 took 74 us, now 69).  Chunk c (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor 16 neighbouring lanes, which read the same chunk of different
-// rows, meet in a bank.
+// to a row, 2047 x 4096 x 11008 took 74 us, now 69).  Chunk c (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor
+// 16 neighbouring lanes, which read the same chunk of different rows, meet in a bank.
+//
+// What bounds it: the matrix instructions alone, operands of random data in registers, make 6.6 PFLOP/s on this card at the clock its power allows (9.8 on
+// zeros); here 3.4 (4.1 on zeros).  Left out one by one (zeros): scales' way to LDS a tenth, codes' way to LDS a tenth, their requests a sixth of the time.
 template <int F>
 struct TileShape {
     static constexpr int kRows = 64 * F;                             // of W and of X
@@ -146,8 +149,6 @@ struct TileShape {
     static constexpr int kLds = 2 * kStageBytes + 2 * kScaleGroupBytes;
     static_assert(kRows / 2 * kPitch <= kLds, "half a tile of sums fits");
 };
-
-typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 
 // Where tile p of the order lies.  Workgroups are handed to the eight XCDs in turn: each takes a contiguous range of the order, which goes through bands of
 // eight tiles of W, so that the tiles in flight on an XCD share rows in its L2.
@@ -160,42 +161,30 @@ struct TileOrder {
     }
 };
 
-// R / 2 rows of R sums in LDS to y, a quarter of them to each of four waves.
-template <int TYPE, int R, bool VEC>
+// R / 2 rows of R sums in LDS to y of any alignment, a quarter of them to each of four waves.
+template <int TYPE, int R>
 __device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds, int pitch, long long m0, long long t0, int wave, int lane) {
     typedef typename MxType<TYPE>::value value;
     constexpr int E = 16 / sizeof(value), kLanes = R / E;     // elements of a 16-byte store, lanes to a row
-    if (VEC && m0 + R <= g.M) {
+    if (m0 + R <= g.M && (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy % E == 0) {
         typedef value vec __attribute__((ext_vector_type(E)));
         const int row0 = R / 8 * wave + lane / kLanes, col = E * (lane % kLanes);
-        auto rows = [&](auto add) {                                  // a loop for each: one that does both loses the kind of its stores
 #pragma unroll 4
-            for (int i = 0; i < R / 8; i += 64 / kLanes) {
-                const int row = row0 + i;
-                if (t0 + row >= g.T) continue;
-                vec* y = reinterpret_cast<vec*>(static_cast<value*>(g.y) + (t0 + row) * g.ldy + m0 + col);
-                const float* s = reinterpret_cast<const float*>(lds + row * pitch) + col;
-                float v[E];
+        for (int i = 0; i < R / 8; i += 64 / kLanes) {
+            const int row = row0 + i;
+            if (t0 + row >= g.T) continue;
+            vec* y = reinterpret_cast<vec*>(static_cast<value*>(g.y) + (t0 + row) * g.ldy + m0 + col);
+            const float* s = reinterpret_cast<const float*>(lds + row * pitch) + col;
+            vec v = {};
+            if (g.accumulate) v = *y;
 #pragma unroll
-                for (int k = 0; k < E; k += 4) {
-                    const f32x4 t = *reinterpret_cast<const f32x4*>(s + k);
-                    v[k] = t.x; v[k + 1] = t.y; v[k + 2] = t.z; v[k + 3] = t.w;
-                }
-                vec out;
-                if constexpr (decltype(add)::value) {
-                    const vec old = *y;
+            for (int k = 0; k < E; k += 4) {
+                const f32x4 t = *reinterpret_cast<const f32x4*>(s + k);
 #pragma unroll
-                    for (int k = 0; k < E; ++k) out[k] = (value)((float)old[k] + v[k]);
-                    *y = out;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < E; ++k) out[k] = (value)v[k];
-                    __builtin_nontemporal_store(out, y);                 // 100 -> 84 us for 4096 x 16384 results of 1024 columns
-                }
+                for (int j = 0; j < 4; ++j) v[k + j] = (value)((float)v[k + j] + t[j]);
             }
-        };
-        if (g.accumulate) rows(std::true_type{});
-        else rows(std::false_type{});
+            *y = v;
+        }
     } else {
         for (int i = 0; i < R / 8; ++i) {
             const int row = R / 8 * wave + i;
@@ -209,9 +198,26 @@ __device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds,
     }
 }
 
-// SHORT: fewer than 512 columns, so four dwords of scales are more than a row holds and are fetched one by one (5120 x 5120 results of 384 columns in fp32:
+// d[4 p + w] of lane c of four, swapped to d[4 c + w] of lane p.
+__device__ __forceinline__ void quad_transpose(u32 (&d)[16], int c) {
+    auto swap = [&](auto ctrl, int bit) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if (e >> 2 & bit) continue;
+            u32 &a = d[e], &b = d[e + 4 * bit];
+            const u32 from_a = __builtin_amdgcn_mov_dpp((int)a, decltype(ctrl)::value, 0xf, 0xf, true), from_b = __builtin_amdgcn_mov_dpp((int)b, decltype(ctrl)::value, 0xf, 0xf, true);
+            const u32 new_a = c & bit ? from_b : a, new_b = c & bit ? b : from_a;
+            a = new_a;
+            b = new_b;
+        }
+    };
+    swap(std::integral_constant<int, 0xb1>{}, 1);                    // lanes 1 0 3 2
+    swap(std::integral_constant<int, 0x4e>{}, 2);                    // lanes 2 3 0 1
+}
+
+// DIRECT: y is only written, in rows of whole aligned 16 bytes.  SHORT: fewer than 512 columns, so four dwords of scales are more than a row holds and are fetched one by one (5120 x 5120 results of 384 columns in fp32:
 // 30 us, 58 with the kernel for few rows).
-template <int TYPE, int F, bool VEC, bool SHORT>
+template <int TYPE, int F, bool DIRECT, bool SHORT>
 __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGemmArgs g, TileOrder order, int K) {
     typedef TileShape<F> S;
     constexpr int R = S::kRows, kStageBytes = S::kStageBytes, kScaleGroupBytes = S::kScaleGroupBytes, NP = S::kPieces;
@@ -234,12 +240,19 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
     const char *codes, *scales;
     u32 off[NP], wr[2];
     int last;
+    // Position 32 block + at of an operand's part of LDS holds that row of it, and for W the row for which a lane's 16 sums of a 32-row operand are neighbours in
+    // y, and beside those of the other half of the wave (fp32) or of the next operand (16 bits): 64 bytes.
+    constexpr bool kPairs = sizeof(typename MxType<TYPE>::value) == 2;
+    auto row_at = [&](int block, int at) {
+        const int base = kPairs ? 64 * (block >> 1) + 16 * (block & 1) : 32 * block;
+        return mine_w ? base + (kPairs ? 32 : 16) * (at >> 2 & 1) + 4 * (at >> 3) + (at & 3) : 32 * block + at;
+    };
     auto aim = [&]() {                                               // the fetches at the tile (m0, t0)
         codes = static_cast<const char*>(mine_w ? g.w_codes : g.x_codes) + (size_t)(mine_w ? m0 : t0) * cp;
         scales = static_cast<const char*>(mine_w ? g.w_scales : g.x_scales) + (size_t)(mine_w ? m0 : t0) * sp;
         last = (int)min((mine_w ? (long long)g.M - m0 : (long long)g.T - t0) - 1, (long long)R - 1);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) off[i] = (u32)min((int)(row0 + 8 * i + (lane >> 3)), last) * cp + 16 * (lane & 7);
+        for (int i = 0; i < NP; ++i) off[i] = (u32)min((int)row0 + row_at(i >> 2, 8 * (i & 3)) + row_at(0, lane >> 3), last) * cp + 16 * (lane & 7);
     };
 #pragma unroll
     for (int i = 0; i < 2; ++i) wr[i] = wave * (64 * R) + 128 * (8 * i + (lane >> 3)) + 16 * ((lane & 7) ^ chunk_swizzle(8 * i + (lane >> 3)));
@@ -248,20 +261,20 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
     f32x16 acc[F][F];
     i32x4 a0[F], b0[F], a1[F], b1[F], pre[NP];
     u32 ua[F], ub[F], va[F], vb[F];
-    u32x4 spre[F / 2];
+    u32x4 spre[F / 2], spre1[F / 2];
     const int quad = 4 * (lane & 1);                                 // of a row's eight dwords of a group a lane moves four
     // K is a multiple of 128: the upper half of the last stage may lie behind the rows, and repeats the lower one with scales of 2^-127, whose products
     // vanish against every fp32 number
     auto fetch = [&](int st, int i) { pre[i] = *reinterpret_cast<const i32x4*>(codes + (size_t)min(st, nst - 1) * 128 + off[i] - ((lane & 4) && 2 * min(st, nst - 1) + 1 >= ndw ? 64 : 0)); };
     auto put = [&](int st, int i) { *reinterpret_cast<i32x4*>(stage + (st & 1) * kStageBytes + 2048 * (i >> 1) + wr[i & 1]) = pre[i]; };
     // Part g of the scales: half the rows (g even: the first) of group g / 2.
-    auto fetch_scales = [&](int g) {
+    auto fetch_scales = [&](int g, u32x4 (&spre)[F / 2]) {
         const int d = 8 * (g >> 1) + quad;
         int end = last;
         asm volatile("" : "+s"(end));                                // offsets made anew each time: kept, they would be spilled
 #pragma unroll
         for (int i = 0; i < F / 2; ++i) {
-            const u32 row = __umul24(min((int)(row0 + R / 4 * (g & 1) + 32 * i) + (lane >> 1), end), sp);
+            const u32 row = __umul24(min((int)row0 + row_at(F / 2 * (g & 1) + i, 0) + row_at(0, lane >> 1), end), sp);
             if constexpr (SHORT) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) spre[i][j] = *reinterpret_cast<const u32*>(scales + (size_t)(row + 4 * (u32)min(d + j, ndw - 1)));
@@ -270,7 +283,7 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
             }
         }
     };
-    auto put_scales = [&](int g) {
+    auto put_scales = [&](int g, const u32x4 (&spre)[F / 2]) {
         char* b = scale + ((g >> 1) & 1) * kScaleGroupBytes + wave * (16 * R) + (g & 1) * (8 * R);
         const int d = 8 * (g >> 1) + quad, over = max(d + 4 - ndw, 0);   // dwords behind the row's end: so much earlier they were fetched
         const bool drop1 = over & 1, drop2 = over & 2, drop4 = over >= 4;
@@ -347,8 +360,8 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
 #pragma unroll
         for (int i = 3 * F; i < NP; ++i) { put(st + 1, i); fetch(st + 2, i); }
         if (kOdd) {
-            put_scales((st >> 1) + 2);
-            fetch_scales((st >> 1) + 3);
+            put_scales((st >> 1) + 2, spre);
+            fetch_scales((st >> 1) + 3, spre);
         }
         multiply(std::integral_constant<int, 2>{}, a0, b0);
 #pragma unroll
@@ -372,22 +385,22 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto request = [&]() {                                           // the first stage and scales of the tile aimed at
+    auto request = [&]() {                                           // the first stage and group of scales of the tile aimed at
 #pragma unroll
         for (int i = 0; i < NP; ++i) fetch(0, i);
-        fetch_scales(0);
+        fetch_scales(0, spre);
+        fetch_scales(1, spre1);
     };
     aim();
     request();
     while (true) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) put(0, i);
-        put_scales(0);
-        fetch_scales(1);
 #pragma unroll
         for (int i = 0; i < NP; ++i) fetch(1, i);
-        put_scales(1);
-        fetch_scales(2);
+        put_scales(0, spre);
+        put_scales(1, spre1);
+        fetch_scales(2, spre);
 #pragma unroll
         for (int i = 0; i < F; ++i)
 #pragma unroll
@@ -408,22 +421,54 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
             aim();
             request();
         }
-        // Through LDS, half the rows of X at a time, so that whole lines of y are written (eight bytes of sixteen rows to an instruction, straight
-        // from the accumulators, kept the L2 busy with requests for as long as 64 stages of a tile take).
-        constexpr int kPitch = S::kPitch;
-        for (int half = 0; half < 2; ++half) {
-            __syncthreads();
-            if (wt == half) {
+        if constexpr (DIRECT) {
+            // Four lanes exchange their 64 bytes of four rows, so that each instruction writes eight whole lines, with no barrier and while the next
+            // tile's stage is on its way (4096 x 22016 results of 8192 columns: 442 us, 470 through LDS).
+            const int c = lane & 3;
+            typedef typename MxType<TYPE>::value value;
+            typedef value pair __attribute__((ext_vector_type(2)));
+            constexpr int E = 16 / sizeof(value);                    // of a store; M is a multiple of it
+            long long t = t_out + R / 2 * wt + (r & ~3);
+            const long long m = m_out + R / 2 * wm + (kPairs ? 32 : 16) * h + E * c;
+            value* y = static_cast<value*>(g.y) + t * g.ldy + m;
 #pragma unroll
-                for (int i = 0; i < F; ++i)
+            for (int k = 0; k < F; ++k, t += 32, y += 32 * g.ldy) {
 #pragma unroll
-                    for (int k = 0; k < F; ++k)
+                for (int i = 0; i < F; i += 2) {
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4)
-                            *reinterpret_cast<f32x4*>(lds + (32 * k + r) * kPitch + 4 * (R / 2 * wm + 32 * i + 4 * h + 2 * e)) = f32x4{acc[i][k][e], acc[i][k][e + 1], acc[i][k][e + 2], acc[i][k][e + 3]};
+                    for (int s = 0; s < (kPairs ? 1 : 2); ++s) {
+                        u32 d[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if constexpr (!kPairs) d[e] = __float_as_uint(acc[i + s][k][e]);
+                            else d[e] = __builtin_bit_cast(u32, pair{(value)acc[i + (e >> 3)][k][2 * (e & 7)], (value)acc[i + (e >> 3)][k][2 * (e & 7) + 1]});
+                        }
+                        quad_transpose(d, c);
+                        const int at = 32 * (i + s);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (t + j < g.T && m + at < g.M) __builtin_nontemporal_store(u32x4{d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]}, reinterpret_cast<u32x4*>(y + j * g.ldy + at));
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
             }
-            __syncthreads();
-            store_rows<TYPE, R, VEC>(g, lds, kPitch, m_out, t_out + R / 2 * half, wave, lane);
+        } else {
+            // Through LDS, half the rows of X at a time, in fp32 so that what is in y can be added before the sum is rounded.
+            constexpr int kPitch = S::kPitch;
+            for (int half = 0; half < 2; ++half) {
+                __syncthreads();
+                if (wt == half) {
+#pragma unroll
+                    for (int i = 0; i < F; ++i)
+#pragma unroll
+                        for (int k = 0; k < F; ++k)
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4)
+                                *reinterpret_cast<f32x4*>(lds + (32 * k + r) * kPitch + 4 * (R / 2 * wm + (kPairs ? 64 * (i >> 1) + 32 * h + 16 * (i & 1) : 32 * i + 16 * h) + e)) = f32x4{acc[i][k][e], acc[i][k][e + 1], acc[i][k][e + 2], acc[i][k][e + 3]};
+                }
+                __syncthreads();
+                store_rows<TYPE, R>(g, lds, kPitch, m_out, t_out + R / 2 * half, wave, lane);
+            }
         }
         if (!more) break;
         __syncthreads();
@@ -437,8 +482,8 @@ hipError_t gemm_tiles(const MxGemmArgs& g, int K, hipStream_t s) {
     constexpr int R = TileShape<F>::kRows;
     const TileOrder order = {(int)(((long long)g.M + R - 1) / R), (int)(((long long)g.T + R - 1) / R), R};
     const unsigned grid = F == 4 ? 256 : 512;                        // one workgroup to a compute unit, or two
-    const bool vec = (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy * mx_type_size(TYPE) % 16 == 0;
-    if (vec) mx_gemm_tile_kernel<TYPE, F, true, SHORT><<<grid, 256, 0, s>>>(g, order, K);
+    const int e = 16 / mx_type_size(TYPE);
+    if (!g.accumulate && (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy % e == 0 && g.M % e == 0) mx_gemm_tile_kernel<TYPE, F, true, SHORT><<<grid, 256, 0, s>>>(g, order, K);
     else mx_gemm_tile_kernel<TYPE, F, false, SHORT><<<grid, 256, 0, s>>>(g, order, K);
     return hipGetLastError();
 }
@@ -456,26 +501,27 @@ hipError_t gemm_few(const MxGemmArgs& g, int K, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Which kernel: the one whose estimate is lowest.  An estimate, in microseconds, is a fixed part and a part per 1024 columns (k) for each round of tiles
-// over the compute units, fitted to measured times: 4096 x 16384 results of 1024 / 8192 columns take 81 / 326 us with tiles of 256 and 79 / 375
-// with 128, 2047 x 4096 of 11008 83 and 67, 301 x 5120 of 5120 42 and 17 (22 with few rows), 128 x 4096 of 11008 29 with 128 and 15 with few rows,
-// 33 x 11008 of 4096 13.4 and 12.
-double cost_of_256(double rows, double others, double k) { return std::ceil(std::ceil(rows / 256) * std::ceil(others / 256) / 256) * (12.6 + 7.6 * k); }
-double cost_of_128(double rows, double others, double k) {
+// Which kernel: the one whose estimate is lowest.  An estimate, in microseconds, is a part for the result (size bytes an element) and a part per 1024 columns (k)
+// for each round of tiles over the compute units, fitted to measured times.  Tiles of 256 / 128, bf16: 4096 x 16384 results of 1024 columns take 79 / 70 us,
+// of 2048 112 / 104, of 8192 313 / 358; 2048 x 16384 of 4096 94 / 100; 2047 x 4096 of 11008 78 / 64; fp32: 4096 x 11008 of 2047 102 / 91.  128 / few rows: 301 x
+// 5120 of 5120 15 / 22, 128 x 4096 of 11008 29 / 15, 33 x 11008 of 4096 13.4 / 12.
+double cost_of_256(double rows, double others, double k, int size) { return std::ceil(std::ceil(rows / 256) * std::ceil(others / 256) / 256) * (4.8 + 3.3 * size + 8.3 * k); }
+double cost_of_128(double rows, double others, double k, int size) {
     const double tiles = std::ceil(rows / 128) * std::ceil(others / 128);
-    return tiles <= 256 ? 4.5 + 2.4 * k : std::ceil(tiles / 512) * (4.2 + 5.2 * k);
+    return tiles <= 256 ? 4.0 + 2.5 * k : std::ceil(tiles / 512) * (1.6 + 0.9 * size + 5.15 * k);
 }
 double cost_of_few(double rows, double others, double k) { return 5.8 + (0.0026 + 0.0039 * k) * std::ceil(rows / 32) * std::ceil(others / (others <= 32 ? 32 : 64)); }
 
 template <int TYPE>
 hipError_t gemm(const MxGemmArgs& g, hipStream_t s) {
     const int K = mx_padded(g.N);
-    const double k = K / 1024.0, cost2 = cost_of_128(g.M, g.T, k), few = cost_of_few(g.M, g.T, k);
+    const int size = mx_type_size(TYPE);
+    const double k = K / 1024.0, cost2 = cost_of_128(g.M, g.T, k, size), few = cost_of_few(g.M, g.T, k);
     if (K <= 1 << 24) {                                              // offsets inside a tile are 32 bits
         if (K < 512) {
             if (cost2 < few) return gemm_tiles<TYPE, 2, true>(g, K, s);
         } else {
-            const double cost4 = cost_of_256(g.M, g.T, k);
+            const double cost4 = cost_of_256(g.M, g.T, k, size);
             if (std::min(cost4, cost2) < few) return cost4 < cost2 ? gemm_tiles<TYPE, 4, false>(g, K, s) : gemm_tiles<TYPE, 2, false>(g, K, s);
         }
     }

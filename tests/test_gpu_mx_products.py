@@ -169,6 +169,28 @@ def test_gemm_of_many_rows(T, M, N, kind):
     assert bool((big[:, M:] == 3.0).all()) and bool((big[T] == 3.0).all())
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("T,M,N", [(1030, 2056, 1500), (2300, 4104, 5000), (1027, 5000, 100), (4099, 2064, 260), (513, 4095, 1024)])
+def test_gemm_of_many_rows_aligned(T, M, N, kind):
+    """rows of y that start at 16 bytes, written and added to, with ends inside a tile; a tail of the rows is left as it was"""
+    import torch
+    import paper_2306_07629_amd as sq
+    print(f"mx gemm aligned {T}x{M}x{N} {kind}", flush=True)
+    rng = np.random.default_rng(T + M + N)
+    x, xv = packed(T, N, rng, 4, 124)
+    w, wv = packed(M, N, rng, 6, 119)
+    want, S = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    big = torch.full((T + 1, M + 16 - M % 8), 3.0, dtype=dtype_of(kind), device="cuda")
+    part = big[:T, :M]
+    sq.mx_gemm(x, w, y=part)
+    first = host(part)
+    close(first, want, S, N, kind)
+    assert torch.equal(sq.mx_gemm(x, w, dtype_of(kind)), part)
+    sq.mx_gemm(x, w, y=part, accumulate=True)
+    close(host(part), first + want, S, N, kind)
+    assert bool((big[:, M:] == 3.0).all()) and bool((big[T] == 3.0).all())
+
+
 @pytest.mark.parametrize("T,M,N", [(33, 65, 300), (300, 270, 1152), (2100, 4100, 640)])
 def test_gemm_ends_of_the_ranges(T, M, N):
     """NaN blocks reach their rows only; scales whose products leave fp16 or fp32 give infinities where the definition does"""

@@ -7,11 +7,17 @@ import torch
 from . import binding
 
 ROW = 128       # columns a packed row is padded to
+MOST_ROWS, MOST_COLUMNS = 2**31 - 1, 2**31 - 128     # the library counts in 32 bits
 _TYPES = {torch.float16: binding.TYPE_F16, torch.bfloat16: binding.TYPE_BF16, torch.float32: binding.TYPE_F32}
 
 
 def _refuse(name, message):
     raise binding.SqllmError(binding.STATUS_NAMES.index(name), message)
+
+
+def _need_size(M, N):
+    if not (0 <= M <= MOST_ROWS and 0 < N <= MOST_COLUMNS):
+        _refuse("SQLLM_ERR_SHAPE", f"a packed matrix of {M} x {N}")
 
 
 def _call(device, fn, *args):
@@ -61,8 +67,7 @@ class MxMatrix:
     __slots__ = ("M", "N", "codes", "scales")
 
     def __init__(self, M: int, N: int, codes: torch.Tensor, scales: torch.Tensor):
-        if M < 0 or N <= 0:
-            _refuse("SQLLM_ERR_SHAPE", f"a packed matrix of {M} x {N}")
+        _need_size(M, N)
         padded = -(-N // ROW) * ROW
         for t, what, width in ((codes, "codes", padded // 2), (scales, "scales", padded // 32)):
             _need(t, what, codes, torch.uint8, (M, width))
@@ -72,8 +77,7 @@ class MxMatrix:
 
     @staticmethod
     def empty(M, N, device):
-        if M < 0 or N <= 0:
-            _refuse("SQLLM_ERR_SHAPE", f"a packed matrix of {M} x {N}")
+        _need_size(M, N)
         padded = -(-N // ROW) * ROW
         m = object.__new__(MxMatrix)
         m.M, m.N = M, N

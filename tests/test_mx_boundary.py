@@ -86,6 +86,12 @@ def test_packed_matrices_are_checked():
     assert status(sq.MxMatrix, 3, 130, torch.zeros((3, 128), dtype=torch.uint8), fake(3, 8)) == "SQLLM_ERR_DEVICE"
 
 
+@pytest.mark.parametrize("M,N", [(1 << 31, 128), (1 << 32, 1), (3, (1 << 31) - 127), (1, (1 << 32) + 128), (-1, 128), (0, 0)])
+def test_sizes_beyond_the_librarys_are_refused(M, N):
+    for make in (lambda: sq.MxMatrix.empty(M, N, "cpu"), lambda: sq.MxMatrix(M, N, fake(1, 64), fake(1, 4))):
+        assert status(make) == "SQLLM_ERR_SHAPE"
+
+
 def test_operands_are_checked():
     f16 = dict(dtype=torch.float16)
     assert status(sq.mx_quantize, torch.zeros(3, 4)) == "SQLLM_ERR_DEVICE"

@@ -239,7 +239,7 @@ int sqllm_quantize_layer_noalloc(int M, int N, int bits, int max_iter, const voi
  *                      Either pair may be NULL, not both; w is read once for both.  Rounding and scales are exact: the result is a pure function of w.
  * sqllm_mx_dequantize  writes code * 2^(s - 127) as `type` to w_out [M][N], stride ldw; rounded once (fp16: beyond 65504 to Inf; exact where the type holds the value).
  * sqllm_mx_gemv        y = W x (accumulate == 0) or y = fp16( fp32(y) + W x ): x fp16 [N][B], y fp16 [M][B], B = 1..16, N and the alignments of x and y as for sqllm_lut_gemv, so that
- *                      sqllm_csr_spmv can add a sparse term of the same layer to y.  Products are exact, sums in fp32.
+ *                      sqllm_csr_spmv can add a sparse term of the same layer to y.  Products are exact, sums in fp32.  An Inf or NaN of x makes its column of y, and no other, Inf or NaN.
  * sqllm_mx_gemm        y[t][i] = sum_j X[t][j] W[i][j] of two packed matrices: X has T rows, W has M, both N columns; y is `type` [T][M] with row stride ldy.  accumulate != 0 adds to
  *                      what y holds (read as `type`, added in fp32).  Products are exact, sums in fp32; one rounding to `type`.  T == 0 -> SQLLM_OK.
  *                      With X the tokens and W a layer this is its forward pass.  Backward, with dY [T][M]: dX = sqllm_mx_gemm of dY's rows and W's transpose, dW = of dY's transpose and X's transpose.

@@ -561,12 +561,18 @@ hipError_t gemv_batch(const MxGemvArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_mx_gemv(const MxGemvArgs& a, hipStream_t s) {
-    switch (a.B) {
-        case 1: return gemv_few<1, 4>(a, s);
-        case 2: return gemv_few<2, 4>(a, s);
-        default: return gemv_batch<SQLLM_MAX_BATCH>(a, s);
+hipError_t launch_mx_gemv(const MxGemvArgs& all, hipStream_t s) {
+    constexpr int kMostRows = 1 << 28;                               // of a launch, whose threads are counted in 32 bits
+    for (long long r0 = 0; r0 < all.M; r0 += kMostRows) {
+        MxGemvArgs a = all;
+        a.M = (int)std::min<long long>(all.M - r0, kMostRows);
+        a.codes = static_cast<const char*>(all.codes) + r0 * mx_row_code_bytes(a.N);
+        a.scales = static_cast<const char*>(all.scales) + r0 * mx_row_scale_bytes(a.N);
+        a.y = static_cast<half_t*>(all.y) + r0 * a.B;
+        const hipError_t e = a.B == 1 ? gemv_few<1, 4>(a, s) : a.B == 2 ? gemv_few<2, 4>(a, s) : gemv_batch<SQLLM_MAX_BATCH>(a, s);
+        if (e != hipSuccess) return e;
     }
+    return hipSuccess;
 }
 
 }  // namespace sqllm

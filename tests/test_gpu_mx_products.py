@@ -301,6 +301,70 @@ def test_dense_and_sparse_layer(B):
     assert torch.equal(packed_rest.dequantize(torch.float16).float() != 0, torch.from_numpy(W != 0).cuda())
 
 
+@pytest.mark.parametrize("B", [1, 3])
+def test_gemv_of_more_rows_than_a_launch(B):
+    """2^28 + 37 rows: the last 64 hold numbers, the others zeros"""
+    import torch
+    import paper_2306_07629_amd as sq
+    M, N = (1 << 28) + 37, 128
+    rng = np.random.default_rng(B)
+    tail, v = packed(64, N, rng)
+    w = sq.MxMatrix(M, N, torch.zeros((M, 64), dtype=torch.uint8, device="cuda"), torch.full((M, 4), 120, dtype=torch.uint8, device="cuda"))
+    w.codes[-64:], w.scales[-64:] = tail.codes, tail.scales
+    x = torch.from_numpy(rng.normal(size=(N, B)).astype(np.float16)).cuda()
+    y = sq.mx_gemv(w, x)
+    xh = host(x)
+    close(host(y[-64:]), v @ xh, np.abs(v) @ np.abs(xh), N)
+    assert not bool(y[:-64].any())
+
+
+@pytest.mark.parametrize("T,M,N,kind", [(33100, 33001, 100, "f32"), (46400, 46408, 130, "bf16")])
+def test_gemm_with_a_result_beyond_four_gigabytes(T, M, N, kind):
+    import torch
+    import paper_2306_07629_amd as sq
+    rng = np.random.default_rng(T)
+    x, xv = packed(T, N, rng, 4, 124)
+    w, wv = packed(M, N, rng, 6, 119)
+    y = sq.mx_gemm(x, w, dtype_of(kind))
+    for rows, cols in ((slice(0, 70), slice(0, 300)), (slice(T - 70, T), slice(M - 300, M)), (slice(T // 2, T // 2 + 70), slice(0, 300))):
+        close(host(y[rows, cols]), xv[rows] @ wv[cols].T, np.abs(xv[rows]) @ np.abs(wv[cols]).T, N, kind)
+
+
+@pytest.mark.parametrize("M,N", [(40, 300), (700, 1152), (2200, 640)])
+def test_gemm_of_a_matrix_with_itself(M, N):
+    import torch
+    import paper_2306_07629_amd as sq
+    w, v = packed(M, N, np.random.default_rng(M))
+    got = sq.mx_gemm(w, w, torch.float32)
+    close(host(got), v @ v.T, np.abs(v) @ np.abs(v).T, N, "f32")
+    other = sq.MxMatrix(M, N, w.codes.clone(), w.scales.clone())
+    assert torch.equal(sq.mx_gemm(w, other, torch.float32), got)
+
+
+def test_two_streams_at_once():
+    """calls of every operator that run side by side on two streams, sharing their weights"""
+    import torch
+    import paper_2306_07629_amd as sq
+    rng = np.random.default_rng(12)
+    w, _ = packed(1200, 2048, rng)
+    xs = [torch.from_numpy(rng.normal(size=(T, 2048)).astype(np.float16)).cuda() for T in (40, 600)]
+    cols = [torch.from_numpy(rng.normal(size=(2048, B)).astype(np.float16)).cuda() for B in (1, 7)]
+    def step(i):
+        q, q_t = sq.mx_quantize(xs[i], "both")
+        return [q.codes, q_t.codes, sq.mx_gemm(q, w), sq.mx_gemv(w, cols[i]), q.dequantize(torch.float32), sq.mx_gemm(q_t, q_t, torch.float32)]
+    want = [step(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [None, None]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = step(i)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want[i])), i
+
+
 def test_streams_graphs_and_repeated_calls():
     """every operator on another stream than the current one's and in a replayed graph, with eager work between the replays"""
     import torch

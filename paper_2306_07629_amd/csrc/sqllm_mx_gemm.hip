@@ -161,11 +161,11 @@ struct TileOrder {
     }
 };
 
-// R / 2 rows of R sums in LDS to y of any alignment, a quarter of them to each of four waves.
+// R / 2 rows of R sums in LDS added to y, a quarter of them by each of four waves.
 template <int TYPE, int R>
-__device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds, int pitch, long long m0, long long t0, int wave, int lane) {
+__device__ __forceinline__ void add_rows(const MxGemmArgs& g, const char* lds, int pitch, long long m0, long long t0, int wave, int lane) {
     typedef typename MxType<TYPE>::value value;
-    constexpr int E = 16 / sizeof(value), kLanes = R / E;     // elements of a 16-byte store, lanes to a row
+    constexpr int E = 16 / sizeof(value), kLanes = R / E;     // elements of 16 bytes, lanes to a row
     if (m0 + R <= g.M && (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy % E == 0) {
         typedef value vec __attribute__((ext_vector_type(E)));
         const int row0 = R / 8 * wave + lane / kLanes, col = E * (lane % kLanes);
@@ -175,8 +175,7 @@ __device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds,
             if (t0 + row >= g.T) continue;
             vec* y = reinterpret_cast<vec*>(static_cast<value*>(g.y) + (t0 + row) * g.ldy + m0 + col);
             const float* s = reinterpret_cast<const float*>(lds + row * pitch) + col;
-            vec v = {};
-            if (g.accumulate) v = *y;
+            vec v = *y;
 #pragma unroll
             for (int k = 0; k < E; k += 4) {
                 const f32x4 t = *reinterpret_cast<const f32x4*>(s + k);
@@ -193,7 +192,7 @@ __device__ __forceinline__ void store_rows(const MxGemmArgs& g, const char* lds,
             const float* s = reinterpret_cast<const float*>(lds + row * pitch);
 #pragma unroll
             for (int c = lane; c < R; c += 64)
-                if (m0 + c < g.M) y[c] = (value)(g.accumulate ? (float)y[c] + s[c] : s[c]);
+                if (m0 + c < g.M) y[c] = (value)((float)y[c] + s[c]);
         }
     }
 }
@@ -215,9 +214,14 @@ __device__ __forceinline__ void quad_transpose(u32 (&d)[16], int c) {
     swap(std::integral_constant<int, 0x4e>{}, 2);                    // lanes 2 3 0 1
 }
 
-// DIRECT: y is only written, in rows of whole aligned 16 bytes.  SHORT: fewer than 512 columns, so four dwords of scales are more than a row holds and are fetched one by one (5120 x 5120 results of 384 columns in fp32:
+// What becomes of the sums: added to y, or written to it, past the caches or through them.  Rows of y that are not aligned to 16 bytes share
+// lines, which gather in the caches: 4096 x 8191 results, bf16 of 4096 columns 105 us, past the caches 114, fp32 of 1024 60 and 78; tiles of 128 in 16 bits write
+// shorter pieces sooner after one another and do not gain, of 1024 columns 50 and 44.  Through LDS an element at a time they took 129, 65 and 59.
+enum Out { kAdd, kStream, kCached };
+
+// SHORT: fewer than 512 columns, so four dwords of scales are more than a row holds and are fetched one by one (5120 x 5120 results of 384 columns in fp32:
 // 30 us, 58 with the kernel for few rows).
-template <int TYPE, int F, bool DIRECT, bool SHORT>
+template <int TYPE, int F, Out OUT, bool SHORT>
 __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGemmArgs g, TileOrder order, int K) {
     typedef TileShape<F> S;
     constexpr int R = S::kRows, kStageBytes = S::kStageBytes, kScaleGroupBytes = S::kScaleGroupBytes, NP = S::kPieces;
@@ -423,13 +427,13 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
             aim();
             request();
         }
-        if constexpr (DIRECT) {
+        if constexpr (OUT != kAdd) {
             // Four lanes exchange their 64 bytes of four rows, so that each instruction writes eight whole lines, with no barrier and while the next
             // tile's stage is on its way (4096 x 22016 results of 8192 columns: 442 us, 470 through LDS).
             const int c = lane & 3;
             typedef typename MxType<TYPE>::value value;
             typedef value pair __attribute__((ext_vector_type(2)));
-            constexpr int E = 16 / sizeof(value);                    // of a store; M is a multiple of it
+            constexpr int E = 16 / sizeof(value);                    // of a store
             long long t = t_out + R / 2 * wt + (r & ~3);
             const long long m = m_out + R / 2 * wm + (kPairs ? 32 : 16) * h + E * c;
             value* y = static_cast<value*>(g.y) + t * g.ldy + m;
@@ -449,13 +453,31 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
                         const int at = 32 * (i + s);
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            if (t + j < g.T && m + at < g.M) __builtin_nontemporal_store(u32x4{d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]}, reinterpret_cast<u32x4*>(y + j * g.ldy + at));
+                            if (t + j < g.T) {
+                                value* dst = y + j * g.ldy + at;
+                                u32x4 v = {d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]};
+                                const long long left = g.M - (m + at);
+                                if (left >= E) {
+                                    if constexpr (OUT == kStream && kPairs) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_a2*>(dst));
+                                    else if constexpr (OUT == kStream) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_a4*>(dst));
+                                    else if constexpr (kPairs) *reinterpret_cast<u32x4_a2*>(dst) = v;
+                                    else *reinterpret_cast<u32x4_a4*>(dst) = v;
+                                } else {
+#pragma unroll 1
+                                    for (int e = 0; e < left; ++e) {
+                                        dst[e] = __builtin_bit_cast(value, (typename std::conditional<kPairs, uint16_t, u32>::type)v.x);
+                                        constexpr int kShift = 8 * sizeof(value) % 32;
+                                        if constexpr (kPairs) v = u32x4{__builtin_amdgcn_alignbit(v.y, v.x, kShift), __builtin_amdgcn_alignbit(v.z, v.y, kShift), __builtin_amdgcn_alignbit(v.w, v.z, kShift), v.w >> kShift};
+                                        else v = u32x4{v.y, v.z, v.w, 0u};
+                                    }
+                                }
+                            }
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
         } else {
-            // Through LDS, half the rows of X at a time, in fp32 so that what is in y can be added before the sum is rounded.
+            // Through LDS, half the rows of X at a time, so that y is read and written in whole lines.
             constexpr int kPitch = S::kPitch;
             for (int half = 0; half < 2; ++half) {
                 __syncthreads();
@@ -469,7 +491,7 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
                                 *reinterpret_cast<f32x4*>(lds + (32 * k + r) * kPitch + 4 * (R / 2 * wm + (kPairs ? 64 * (i >> 1) + 32 * h + 16 * (i & 1) : 32 * i + 16 * h) + e)) = f32x4{acc[i][k][e], acc[i][k][e + 1], acc[i][k][e + 2], acc[i][k][e + 3]};
                 }
                 __syncthreads();
-                store_rows<TYPE, R>(g, lds, kPitch, m_out, t_out + R / 2 * half, wave, lane);
+                add_rows<TYPE, R>(g, lds, kPitch, m_out, t_out + R / 2 * half, wave, lane);
             }
         }
         if (!more) break;
@@ -484,9 +506,11 @@ hipError_t gemm_tiles(const MxGemmArgs& g, int K, hipStream_t s) {
     constexpr int R = TileShape<F>::kRows;
     const TileOrder order = {(int)(((long long)g.M + R - 1) / R), (int)(((long long)g.T + R - 1) / R), R};
     const unsigned grid = F == 4 ? 256 : 512;                        // one workgroup to a compute unit, or two
-    const int e = 16 / mx_type_size(TYPE);
-    if (!g.accumulate && (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy % e == 0 && g.M % e == 0) mx_gemm_tile_kernel<TYPE, F, true, SHORT><<<grid, 256, 0, s>>>(g, order, K);
-    else mx_gemm_tile_kernel<TYPE, F, false, SHORT><<<grid, 256, 0, s>>>(g, order, K);
+    constexpr int e = 16 / (TYPE == SQLLM_F32 ? 4 : 2);
+    constexpr Out kUnaligned = F == 2 && TYPE != SQLLM_F32 ? kStream : kCached;
+    if (g.accumulate) mx_gemm_tile_kernel<TYPE, F, kAdd, SHORT><<<grid, 256, 0, s>>>(g, order, K);
+    else if ((reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy % e == 0) mx_gemm_tile_kernel<TYPE, F, kStream, SHORT><<<grid, 256, 0, s>>>(g, order, K);
+    else mx_gemm_tile_kernel<TYPE, F, kUnaligned, SHORT><<<grid, 256, 0, s>>>(g, order, K);
     return hipGetLastError();
 }
 

@@ -38,17 +38,18 @@ template <int TYPE, int AHEAD>
 __global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(MxQuantArgs a, RowShape rs, size_t code_pitch, size_t scale_pitch) {
     const int chunk = (int)(blockIdx.x << rs.log_tpr) + (int)(threadIdx.x & ((1u << rs.log_tpr) - 1));
     if (chunk >= rs.chunks) return;                                  // whole quads: chunks is a multiple of 16
-    const int rows = kThreads >> rs.log_tpr, j0 = 8 * chunk, left = a.N - j0;
+    const int rows = kThreads >> rs.log_tpr, j0 = 8 * chunk;
     typedef typename MxType<TYPE>::value value;
     const long long step = (long long)gridDim.y * rows;
     for (long long r = (long long)blockIdx.y * rows + (threadIdx.x >> rs.log_tpr); r < a.M; r += AHEAD * step) {
         MxEight<TYPE> e[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
-            if (r + k * step < a.M) e[k].load(static_cast<const value*>(a.w) + (r + k * step) * a.ldw + j0, left, chunk == 0);
+            if (r + k * step < a.M) e[k].load(static_cast<const value*>(a.w) + (r + k * step) * a.ldw, j0, a.N);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             if (r + k * step >= a.M) break;
+            e[k].settle(j0, a.N);
             const u32 byte = mx_scale_byte(mx_magnitude<TYPE>(quad_max(e[k].top())));
             reinterpret_cast<u32*>(static_cast<char*>(a.codes) + (r + k * step) * code_pitch)[chunk] = e[k].pack(byte);
             if ((chunk & 3) == 0) (static_cast<uint8_t*>(a.scales) + (r + k * step) * scale_pitch)[chunk >> 2] = (uint8_t)byte;
@@ -105,14 +106,20 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs 
     const long long m0 = (long long)(at / wide) * kTile;
     const int n0 = (8 * band + at % wide) * kTile, chunk = tid & 15;
     MxEight<TYPE> in[kTile / 16];                                    // all of a thread's share on its way before the first is used
+    const value* const w = static_cast<const value*>(a.w);
+    if (a.N >= 8) {
+        const int j = min(n0 + 8 * chunk, a.N - 8);
 #pragma unroll
-    for (int p = 0; p < kTile / 16; ++p) {
-        const int row = 16 * p + (tid >> 4), left = m0 + row < a.M ? a.N - (n0 + 8 * chunk) : 0;
-        in[p].load(static_cast<const value*>(a.w) + (m0 + row) * a.ldw + n0 + 8 * chunk, left, n0 + chunk == 0);
+        for (int p = 0; p < kTile / 16; ++p) in[p].load(w + min(m0 + 16 * p + (tid >> 4), (long long)a.M - 1) * a.ldw + j);
+    } else {
+#pragma unroll
+        for (int p = 0; p < kTile / 16; ++p) in[p].load_some(w + min(m0 + 16 * p + (tid >> 4), (long long)a.M - 1) * a.ldw, chunk == 0 ? a.N : 0);
     }
 #pragma unroll
     for (int p = 0; p < kTile / 16; ++p) {
         const int row = 16 * p + (tid >> 4);
+        in[p].settle(n0 + 8 * chunk, a.N);
+        if (m0 + row >= a.M) in[p].clear();
         in[p].to_lds(tile + row * kPitch + chunk * D);
         if (ROWS) {
             const u32 byte = mx_scale_byte(mx_magnitude<TYPE>(quad_max(in[p].top())));

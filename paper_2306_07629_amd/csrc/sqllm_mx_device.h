@@ -66,31 +66,44 @@ struct MxEight {
     static constexpr int kDwords = 4 * MxType<TYPE>::kPairDwords;
     u32 v[kDwords];
 
-    // Eight elements from any element's address, with the row going on behind them unless last: dwords from the dword the first one lies in, which holds an
-    // element of the row before it unless `first`.
-    __device__ void load(const void* p, bool first, bool last) {
+    __device__ void load(const void* p) {                            // eight elements from any element's address
         if constexpr (TYPE == SQLLM_F32) {
             const u32x4_a4* s = static_cast<const u32x4_a4*>(p);
             const u32x4 t = s[0], u = s[1];                          // two loads to a line: through the caches
             v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w; v[4] = u.x; v[5] = u.y; v[6] = u.z; v[7] = u.w;
         } else {
-            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-            if ((at & 2) == 0) {
-                const u32x4 t = __builtin_nontemporal_load(static_cast<const u32x4_a4*>(p));
-                v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
-            } else if (first || last) {
-                load_some(p, 8);
-            } else {
-                const u32x4 t = *reinterpret_cast<const u32x4_a4*>(at - 2);
-                const u32 e = *reinterpret_cast<const u32*>(at + 14);
-                v[0] = __builtin_amdgcn_alignbyte(t.y, t.x, 2); v[1] = __builtin_amdgcn_alignbyte(t.z, t.y, 2);
-                v[2] = __builtin_amdgcn_alignbyte(t.w, t.z, 2); v[3] = __builtin_amdgcn_alignbyte(e, t.w, 2);
-            }
+            // gfx950 takes sixteen bytes at any address (dwords that were shifted together: 11008 x 4095 bf16 in both directions 65 us, so 52)
+            const u32x4 t = __builtin_nontemporal_load(static_cast<const u32x4_a2*>(p));
+            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
         }
     }
-    __device__ void load(const void* p, int left, bool first) {      // what there is of them
-        if (left >= 8) load(p, first, left == 8);
-        else load_some(p, max(left, 0));
+    // Eight elements of a row of n from element j on.  Where the row ends before, its last eight are fetched, and settle() moves them: a lane that fetched its few
+    // one by one made its wave wait for all its requests (1999 x 5118 fp16 in both directions 20.2 us, now 10.8).
+    typedef typename MxType<TYPE>::value value;
+    __device__ void load(const value* row, int j, int n) {
+        if (n >= 8) load(row + min(j, n - 8));
+        else load_some(row + j, max(n - j, 0));                      // j = 0 or behind the row
+    }
+    __device__ void settle(int j, int n) {
+        const int by = n >= 8 ? j - (n - 8) : 0;                     // elements too early
+        if (by > 0) {
+            constexpr int kPer = TYPE == SQLLM_F32 ? 1 : 2;          // elements of a dword
+            if (kPer == 2 && (by & 1)) {
+#pragma unroll
+                for (int i = 0; i < kDwords; ++i) v[i] = __builtin_amdgcn_alignbyte(i + 1 < kDwords ? v[i + 1] : 0u, v[i], 2);
+            }
+#pragma unroll
+            for (int s = 1; s < kDwords; s *= 2) {
+                const bool move = by / kPer & s;
+#pragma unroll
+                for (int i = 0; i < kDwords; ++i) v[i] = move ? (i + s < kDwords ? v[i + s] : 0u) : v[i];
+            }
+            if (by >= 8) clear();
+        }
+    }
+    __device__ void clear() {
+#pragma unroll
+        for (int i = 0; i < kDwords; ++i) v[i] = 0u;
     }
     __device__ void load_some(const void* p, int n) {                // the first n (0..8) elements, any alignment; the rest is zero
         if constexpr (TYPE == SQLLM_F32) {
@@ -107,18 +120,9 @@ struct MxEight {
 #pragma unroll
         for (int i = 0; i < kDwords / 4; ++i) reinterpret_cast<u32x4*>(d)[i] = u32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
     }
-    // Past the caches where neighbouring lanes write whole lines with one store (13824 x 5120 to fp16: 41 -> 28 us).
+    // Past the caches: neighbouring lanes write whole lines with one store (13824 x 5120 to fp16: 41 -> 28 us).
     __device__ void store(void* p) const {                           // 16-bit types, to any element's address
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-        if ((at & 2) == 0) {
-            __builtin_nontemporal_store(u32x4{v[0], v[1], v[2], v[3]}, static_cast<u32x4_a4*>(p));
-        } else {
-            typedef u32 u32x3 __attribute__((ext_vector_type(3)));
-            typedef u32x3 u32x3_a4 __attribute__((aligned(4)));
-            *reinterpret_cast<uint16_t*>(at) = (uint16_t)v[0];
-            *reinterpret_cast<u32x3_a4*>(at + 2) = u32x3{__builtin_amdgcn_alignbyte(v[1], v[0], 2), __builtin_amdgcn_alignbyte(v[2], v[1], 2), __builtin_amdgcn_alignbyte(v[3], v[2], 2)};
-            *reinterpret_cast<uint16_t*>(at + 14) = (uint16_t)(v[3] >> 16);
-        }
+        __builtin_nontemporal_store(u32x4{v[0], v[1], v[2], v[3]}, static_cast<u32x4_a2*>(p));
     }
     __device__ void store_some(void* p, int n) const {
         if constexpr (TYPE == SQLLM_F32) {

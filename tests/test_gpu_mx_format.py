@@ -76,6 +76,24 @@ def test_strided_and_unaligned_matrices(ld, offset, kind):
 
 
 @pytest.mark.parametrize("kind", list(KINDS))
+def test_every_end_of_a_row(kind):
+    """rows that end at every place of a lane's eight elements, of one lane and of several, with NaN bits behind them"""
+    import torch
+    import paper_2306_07629_amd as sq
+    for N in (*range(1, 26), *range(120, 138)):
+        for M, ld, offset in ((9, N, 0), (140, N + 3, 1)):
+            bits = bits_of(kind, (M, N), np.random.default_rng(N))
+            v = mx.to_double(bits, kind)
+            rows, columns = sq.mx_quantize(upload(bits, kind, ld, offset), "both")
+            check(rows, v)
+            check(columns, v.T)
+            check(sq.mx_quantize(upload(bits, kind, ld, offset)), v)
+            want = mx.from_double(mx.expand(rows.codes.cpu().numpy(), rows.scales.cpu().numpy(), N), kind)
+            got = rows.dequantize(dtype_of(kind)).view(torch.int32 if kind == "f32" else torch.int16).cpu().numpy().view(UINT[kind])
+            assert np.array_equal(mx.to_double(got, kind), mx.to_double(want, kind), equal_nan=True), (M, N)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
 def test_special_values(kind):
     """one kind of block per pair of rows and columns: zeros of both signs, subnormals, the largest numbers, infinities, NaNs, borders of the scale"""
     import paper_2306_07629_amd as sq

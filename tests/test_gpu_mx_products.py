@@ -191,6 +191,31 @@ def test_gemm_of_many_rows_aligned(T, M, N, kind):
     assert bool((big[:, M:] == 3.0).all()) and bool((big[T] == 3.0).all())
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("T,M,N", [(1030, 2050, 300), (1030, 2050, 600), (2300, 4098, 5000)])
+def test_gemm_into_rows_at_every_alignment(T, M, N, kind):
+    """row lengths and starts at every place of sixteen bytes, for every kernel of many rows"""
+    import torch
+    import paper_2306_07629_amd as sq
+    print(f"mx gemm alignments {T}x{M}x{N} {kind}", flush=True)
+    rng = np.random.default_rng(T + M + N)
+    x, xv = packed(T, N, rng, 4, 124)
+    w, wv = packed(M, N, rng, 6, 119)
+    want, S = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    first = None
+    for less in range(8):
+        m = M - less
+        part = sq.MxMatrix(m, N, w.codes[:m], w.scales[:m])
+        big = torch.full((T, m + less % 3 + 8), 3.0, dtype=dtype_of(kind), device="cuda")
+        y = big[:, less:less + m]
+        sq.mx_gemm(x, part, y=y)
+        if first is None:
+            first = y.clone()
+            close(host(first), want, S, N, kind)
+        assert torch.equal(y, first[:, :m]), less
+        assert bool((big[:, :less] == 3.0).all()) and bool((big[:, less + m:] == 3.0).all()), less
+
+
 @pytest.mark.parametrize("T,M,N", [(33, 65, 300), (300, 270, 1152), (2100, 4100, 640)])
 def test_gemm_ends_of_the_ranges(T, M, N):
     """NaN blocks reach their rows only; scales whose products leave fp16 or fp32 give infinities where the definition does"""

@@ -269,10 +269,12 @@ _mx_call = _mx_first
 
 def _mx(*args):
     status = _mx_call(*args)
-    if status is None:                                                # arguments that only ctypes knows how to take, or to refuse
-        status = _mx_ctypes(*args)
-    if status:
-        _check(status)
+    if status != OK:
+        _mx_not_ok(status, *args)
+
+
+def _mx_not_ok(status, *args):
+    _check(_mx_ctypes(*args) if status is None else status)           # None: arguments that only ctypes knows how to take, or to refuse
 
 
 def sqllm_mx_quantize(M, N, type, w, ldw, codes, scales, codes_t=None, scales_t=None, stream=None):

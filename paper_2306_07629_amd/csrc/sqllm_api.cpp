@@ -496,8 +496,9 @@ int sqllm_mx_dequantize(int M, int N, int type, const void* codes, const void* s
 
 int sqllm_mx_gemv(int M, int N, int B, const void* codes, const void* scales, const void* x, void* y, int accumulate, void* stream) {
     int st;
-    if ((st = check_shape(M, N, B)) || (st = check_mx_packed(codes, scales, "the matrix")) || (st = check_xy(x, y))) return st;
+    if ((st = check_shape(M, N, B))) return st;
     if (M == 0) return SQLLM_OK;
+    if ((st = check_mx_packed(codes, scales, "the matrix")) || (st = check_xy(x, y))) return st;
     if ((st = check_device())) return st;
     const hipError_t e = sqllm::launch_mx_gemv({M, N, B, accumulate, codes, scales, x, y}, static_cast<hipStream_t>(stream));
     return e != hipSuccess ? hip_fail(e, "mx gemv launch") : SQLLM_OK;

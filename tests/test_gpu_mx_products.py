@@ -366,6 +366,18 @@ def test_gemm_of_a_matrix_with_itself(M, N):
     assert torch.equal(sq.mx_gemm(w, other, torch.float32), got)
 
 
+def test_no_rows_and_no_tokens():
+    import torch
+    import paper_2306_07629_amd as sq
+    half = dict(dtype=torch.float16, device="cuda")
+    none = sq.mx_quantize(torch.zeros((0, 256), **half))
+    assert none.codes.shape == (0, 128) and none.dequantize(torch.float32).shape == (0, 256)
+    assert sq.mx_gemv(none, torch.zeros((256, 3), **half)).shape == (0, 3)
+    w = sq.mx_quantize(torch.ones((5, 256), **half))
+    assert sq.mx_linear(torch.zeros((0, 256), **half), w).shape == (0, 5) and sq.mx_gemm(w, none).shape == (5, 0)
+    torch.cuda.synchronize()
+
+
 def test_two_streams_at_once():
     """calls of every operator that run side by side on two streams, sharing their weights"""
     import torch

@@ -58,6 +58,13 @@ def test_empty_problems_are_ok_without_a_device():
     sq.sqllm_mx_gemm(**dict(GEMM, M=0, ldy=0))
 
 
+def test_empty_problems_need_no_addresses():
+    """arrays of no elements have none to give"""
+    none = dict.fromkeys(("w", "codes", "scales", "codes_t", "scales_t", "w_out", "x", "y", "x_codes", "x_scales", "w_codes", "w_scales"))
+    for fn, base, empty in ((sq.sqllm_mx_quantize, QUANT, "M"), (sq.sqllm_mx_dequantize, DEQUANT, "M"), (sq.sqllm_mx_gemv, GEMV, "M"), (sq.sqllm_mx_gemm, GEMM, "M"), (sq.sqllm_mx_gemm, GEMM, "T")):
+        fn(**dict({k: none.get(k, v) for k, v in base.items()}, **{empty: 0}))
+
+
 def test_status_name():
     assert sq.lib().sqllm_status_string(9) == b"SQLLM_ERR_TYPE" and binding.STATUS_NAMES[9] == "SQLLM_ERR_TYPE"
 

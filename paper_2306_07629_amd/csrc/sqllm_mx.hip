@@ -393,13 +393,15 @@ __global__ void __launch_bounds__(kBatchWaves * 64, 2) mx_gemv_batch_kernel(MxGe
     for (int round = 0; round * kBatchWaves * share < total; ++round) {
         const int first = min((round * kBatchWaves + wave) * share, total);   // the wave's first step
         const int n = min(share, total - first);                     // uniform; may be 0
+        long long top = r0;
+        asm volatile("" : "+s"(top));                                // rows' addresses made anew each round: kept, they were spilled, and waited for x on their way back (8192 x 8192 times 5: 15.3 us, now 13.4)
         auto fetch = [&](int g, BatchCodes<NS>& d) {
-            const size_t row = (size_t)min(r0 + 16 * g + r, (long long)a.M - 1);
+            const size_t row = (size_t)min(top + 16 * g + r, (long long)a.M - 1);
             const u32x4* codes = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.codes) + row * (a.N / 2)) + 4 * first + q;
 #pragma unroll
             for (int s = 0; s < NS; ++s)
                 if (s < n) d.c[s] = codes[4 * s];
-            const size_t srow = (size_t)min(r0 + 16 * g + (lane >> 2), (long long)a.M - 1);
+            const size_t srow = (size_t)min(top + 16 * g + (lane >> 2), (long long)a.M - 1);
             const u32* scales = reinterpret_cast<const u32*>(static_cast<const char*>(a.scales) + srow * nb);
 #pragma unroll
             for (int k = 0; k < (NS + 3) / 4; ++k) d.scale[k] = scales[min(first + min(4 * k + (lane & 3), max(n, 1) - 1), total - 1)];
@@ -407,13 +409,24 @@ __global__ void __launch_bounds__(kBatchWaves * 64, 2) mx_gemv_batch_kernel(MxGe
         BatchCodes<NS> ring[RING];
         half8_t xb[NS][4];
         {
-            // x: lane l fetches rows 2 l and 2 l + 1 of a step (B dwords)
+            // x: lane l fetches rows 2 l and 2 l + 1 of a step (B dwords); rows of 4, 8, 12 or 16 need no padding, and the step goes to LDS as it lies, sixteen
+            // neighbouring bytes to a lane (8192 x 8192 times 16: 17.1 us, now 15.4; 4096 x 14336 20.7, now 16.7)
+            constexpr bool kWhole = P == B;
             const u32* x = static_cast<const u32*>(a.x) + (size_t)B * (64 * min(first, total - 1) + lane);
-            constexpr int C = B <= 4 ? NS : 4, EARLY = NS == 8 ? 1 : RING;   // steps of x requested ahead, groups of codes before x is in place: what 256 registers hold
+            constexpr int C = NS * B <= 36 ? NS : 4, EARLY = NS == 8 ? 1 : RING;   // steps of x requested ahead, groups of codes before x is in place: what 256 registers hold
             u32 v[NS][B];
             auto fetch_x = [&](int s) {
+                const int step = min(s, max(n, 1) - 1);
+                if constexpr (kWhole) {
 #pragma unroll
-                for (int i = 0; i < B; ++i) v[s][i] = x[(size_t)B * (64 * min(s, max(n, 1) - 1)) + i];
+                    for (int i = 0; i < B; i += 4) {
+                        const u32x4 t = reinterpret_cast<const u32x4*>(a.x)[(size_t)(16 * B) * (min(first, total - 1) + step) + 16 * i + lane];
+                        v[s][i] = t.x; v[s][i + 1] = t.y; v[s][i + 2] = t.z; v[s][i + 3] = t.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < B; ++i) v[s][i] = x[(size_t)B * (64 * step) + i];
+                }
             };
 #pragma unroll
             for (int s = 0; s < C && s < NS; ++s) fetch_x(s);
@@ -424,16 +437,21 @@ __global__ void __launch_bounds__(kBatchWaves * 64, 2) mx_gemv_batch_kernel(MxGe
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 asm volatile("" ::: "memory");
+                if constexpr (kWhole) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32 row[P / 2];
+                    for (int i = 0; i < B; i += 4) *reinterpret_cast<u32x4*>(stage + 16 * (16 * i + lane)) = u32x4{v[s][i], v[s][i + 1], v[s][i + 2], v[s][i + 3]};
+                } else {
 #pragma unroll
-                    for (int i = 0; i < P / 2; ++i) {
-                        const int at = h * B + 2 * i;                // halves from the lane's first on
-                        row[i] = 2 * i >= B ? 0u : at % 2 == 0 ? v[s][at / 2] : __builtin_amdgcn_alignbyte(at / 2 + 1 < B ? v[s][at / 2 + 1] : 0u, v[s][at / 2], 2);
+                    for (int h = 0; h < 2; ++h) {
+                        u32 row[P / 2];
+#pragma unroll
+                        for (int i = 0; i < P / 2; ++i) {
+                            const int at = h * B + 2 * i;                // halves from the lane's first on
+                            row[i] = 2 * i >= B ? 0u : at % 2 == 0 ? v[s][at / 2] : __builtin_amdgcn_alignbyte(at / 2 + 1 < B ? v[s][at / 2 + 1] : 0u, v[s][at / 2], 2);
+                        }
+#pragma unroll
+                        for (int i = 0; i < P / 4; ++i) *reinterpret_cast<u32x2*>(stage + 2 * P * (2 * lane + h) + 8 * i) = u32x2{row[2 * i], row[2 * i + 1]};
                     }
-#pragma unroll
-                    for (int i = 0; i < P / 4; ++i) *reinterpret_cast<u32x2*>(stage + 2 * P * (2 * lane + h) + 8 * i) = u32x2{row[2 * i], row[2 * i + 1]};
                 }
                 wave_fence();
                 const u32 from = 2 * ((32 * q + (r >> 2)) * P + 4 * (r & 3));

@@ -12,6 +12,8 @@ constexpr int kMxRowUnit = 128;     // elements a packed row is padded to: one s
 constexpr int kMxMaxN = 0x7FFFFF80; // longest row: its padded length is still an int
 
 inline int mx_padded(int n) { return (int)(((long long)n + kMxRowUnit - 1) / kMxRowUnit * kMxRowUnit); }
+// units (or stages) of 256 columns that a packed row of K columns takes; K + 255 leaves an int
+__host__ __device__ inline int mx_units(int K) { return K / 256 + (K % 256 != 0); }
 inline size_t mx_row_code_bytes(int n) { return (size_t)mx_padded(n) / 2; }
 inline size_t mx_row_scale_bytes(int n) { return (size_t)mx_padded(n) / kMxBlock; }
 inline int mx_type_size(int type) { return type == SQLLM_F32 ? 4 : 2; }

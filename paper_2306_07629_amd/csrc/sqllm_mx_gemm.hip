@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kFewMaxWaves * 64, 2) mx_gemm_few_kernel(MxGem
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6, r = lane & 31, h = lane >> 5;
     const long long m0 = 32ll * (blockIdx.x % tiles_m), t0 = (32ll * FT) * (blockIdx.x / tiles_m);
     const size_t cp = K / 2, sp = K / kMxBlock;
-    const int ndw = K / 128, units = (K + 255) / 256;
+    const int ndw = K / 128, units = mx_units(K);
     char* const own = lds + wave * kOwn;
     const char *codes[F][4], *scales[F];                             // rows past the end repeat the last one; their results are not stored
 #pragma unroll
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
     long long m0, t0;
     order.at(p, m0, t0);
     const u32 cp = K / 2, sp = K / kMxBlock;
-    const int ndw = K / 128, nst = (K + 255) / 256;   // dwords of scales of a row, stages
+    const int ndw = K / 128, nst = mx_units(K);   // dwords of scales of a row, stages
     // waves 0, 1 fetch the rows of W, 2, 3 those of X: R / 2 each, eight of them to an instruction; rows past the end repeat the last one
     const bool mine_w = wave < 2;
     const u32 row0 = R / 2 * (wave & 1);
@@ -528,7 +528,7 @@ hipError_t gemm_tiles(const MxGemmArgs& g, int K, hipStream_t s) {
 template <int TYPE, int FT>
 hipError_t gemm_few(const MxGemmArgs& g, int K, hipStream_t s) {
     const long long tiles_m = ((long long)g.M + 31) / 32, tiles = tiles_m * (((long long)g.T + 32 * FT - 1) / (32 * FT));
-    const int waves = std::min(tiles > 256 ? 4 : 8, (K + 255) / 256);
+    const int waves = std::min(tiles > 256 ? 4 : 8, mx_units(K));
     const size_t lds = (size_t)waves * (1 + FT) * 4096;
     if (lds > 65536) {                                               // above what a launch gets without asking
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemm_few_kernel<TYPE, FT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

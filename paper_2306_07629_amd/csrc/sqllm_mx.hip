@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxDequantArgs a
 constexpr int kTile = 128;
 
 template <int TYPE, bool ROWS>
-__global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs a, int tiles_m, int tiles_n, size_t code_pitch, size_t scale_pitch, size_t code_pitch_t, size_t scale_pitch_t) {
+__global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs a, int tiles_m, int tiles_n, int first, size_t code_pitch, size_t scale_pitch, size_t code_pitch_t, size_t scale_pitch_t) {
     typedef typename MxType<TYPE>::value value;
     constexpr int D = MxEight<TYPE>::kDwords, kPitch = kTile / 8 * D;   // dwords of a row
     extern __shared__ __align__(16) u32 tile[];
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs 
     // the XCDs, to which workgroups are handed in turn, take contiguous ranges of the tiles in bands of eight columns of them: neighbours, whose outputs
     // share cache lines, write through the same L2
     const int tiles = tiles_m * tiles_n, xcd = blockIdx.x & 7;
-    const int p = (int)((long long)tiles * xcd >> 3) + (int)(blockIdx.x >> 3);
+    const int p = (int)((long long)tiles * xcd >> 3) + first + (int)(blockIdx.x >> 3);
     if (p >= (int)((long long)tiles * (xcd + 1) >> 3)) return;
     const int band = p / (8 * tiles_m), at = p % (8 * tiles_m), wide = min(tiles_n - 8 * band, 8);
     const long long m0 = (long long)(at / wide) * kTile;
@@ -511,14 +511,18 @@ hipError_t quantize(const MxQuantArgs& a, hipStream_t s) {
         const int tiles_n = mx_padded(a.N) / kTile, tiles_m = mx_padded(a.M) / kTile;
         const size_t cpt = mx_row_code_bytes(a.M), spt = mx_row_scale_bytes(a.M);
         const unsigned lds = kTile * (kTile / 8) * MxEight<TYPE>::kDwords * 4;
-        const dim3 grid((unsigned)(((long long)tiles_m * tiles_n + 7) / 8 * 8));
         if (lds > 65536 - 2048) {                                    // with the scales above what a launch gets without asking
             const hipError_t e = hipFuncSetAttribute(a.codes ? reinterpret_cast<const void*>(&mx_quantize_tile_kernel<TYPE, true>) : reinterpret_cast<const void*>(&mx_quantize_tile_kernel<TYPE, false>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e != hipSuccess) return e;
         }
-        if (a.codes) mx_quantize_tile_kernel<TYPE, true><<<grid, kThreads, lds, s>>>(a, tiles_m, tiles_n, cp, sp, cpt, spt);
-        else mx_quantize_tile_kernel<TYPE, false><<<grid, kThreads, lds, s>>>(a, tiles_m, tiles_n, cp, sp, cpt, spt);
+        constexpr int kMost = 1 << 20;                               // tiles of an XCD in a launch, whose threads are counted in 32 bits
+        const int share = (int)(((long long)tiles_m * tiles_n + 7) / 8);
+        for (int first = 0; first < share; first += kMost) {
+            const unsigned grid = 8u * std::min(share - first, kMost);
+            if (a.codes) mx_quantize_tile_kernel<TYPE, true><<<grid, kThreads, lds, s>>>(a, tiles_m, tiles_n, first, cp, sp, cpt, spt);
+            else mx_quantize_tile_kernel<TYPE, false><<<grid, kThreads, lds, s>>>(a, tiles_m, tiles_n, first, cp, sp, cpt, spt);
+        }
     } else {
         // Four rows ahead where that leaves eight workgroups to a compute unit: 11008 x 4096 fp16 25.2 -> 21.8 us, but 301 x 5120 3.2 -> 3.7.  Not in fp32, where a
         // row is two loads already: 40 -> 43 us.

@@ -38,3 +38,34 @@ def test_product_of_the_widest_rows(N):
         wc[:, N // 2] &= 15 if N % 2 else 0
     y = sq.mx_gemm(sq.MxMatrix(T, N, xc, xs), sq.MxMatrix(M, N, wc, ws), torch.float32)
     assert np.array_equal(y.cpu().numpy().astype(np.float64), want)
+
+
+def same_as_by_rows(packed, w, step=1 << 26):
+    """a packed matrix of w's rows, compared in pieces with the quantisation of those rows alone"""
+    import torch
+    import paper_2306_07629_amd as sq
+    return all(torch.equal(piece.codes, packed.codes[i:i + step]) and torch.equal(piece.scales, packed.scales[i:i + step])
+               for i in range(0, w.shape[0], step) for piece in (sq.mx_quantize(w[i:i + step]),))
+
+
+def test_quantisation_of_the_most_tiles():
+    """a column of 2^31 - 128 numbers in both directions, and the same numbers as a row along the columns: 2^24 - 1 tiles each, in more than one launch"""
+    import torch
+    import paper_2306_07629_amd as sq
+    w = torch.randn((LARGEST, 1), dtype=torch.float16, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    row = w.view(1, LARGEST)
+    by_rows = sq.mx_quantize(row)
+    for i in (0, 1 << 27, 1 << 30, LARGEST - 4096):                      # what the others are compared with, against the definition
+        code, scale = mx.quantize(row[:, i:i + 4096].cpu().numpy().astype(np.float64))
+        assert np.array_equal(by_rows.codes[:, i // 2:i // 2 + 2048].cpu().numpy(), mx.pack(code)) and np.array_equal(by_rows.scales[:, i // 32:i // 32 + 128].cpu().numpy(), scale)
+    print("a column in both directions", flush=True)
+    rows, columns = sq.mx_quantize(w, "both")
+    assert torch.equal(columns.codes, by_rows.codes) and torch.equal(columns.scales, by_rows.scales)
+    assert same_as_by_rows(rows, w)
+    del rows, columns
+    torch.cuda.empty_cache()
+    print("a row along the columns", flush=True)
+    columns = sq.mx_quantize(row, "columns")
+    assert same_as_by_rows(columns, w)
+    del columns, by_rows, w, row
+    torch.cuda.empty_cache()

@@ -568,10 +568,12 @@ template <int B, int NS, int RING>
 hipError_t gemv_batch(const MxGemvArgs& a, int share, hipStream_t s) {
     // one workgroup to a compute unit, as long as the partial sums of its rows fit
     const long long groups = ((long long)a.M + 15) / 16;
-    const int G = (int)std::min<long long>(8, (groups + 255) / 256);
-    const size_t lds = (size_t)kBatchWaves * (batch_stage_bytes(B) + G * 1024);
-    if (lds > 65536) {                                               // above what a launch gets without asking
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemv_batch_kernel<B, NS, RING>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    constexpr int kMostGroups = 8;
+    const int G = (int)std::min<long long>(kMostGroups, (groups + 255) / 256);
+    auto lds_of = [](int G) { return (size_t)kBatchWaves * (batch_stage_bytes(B) + G * 1024); };
+    const size_t lds = lds_of(G);
+    if (lds > 65536) {                                               // above what a launch gets without asking; always the most, as another thread may be between this and its launch
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemv_batch_kernel<B, NS, RING>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_of(kMostGroups));
         if (e != hipSuccess) return e;
     }
     mx_gemv_batch_kernel<B, NS, RING><<<dim3((unsigned)((groups + G - 1) / G)), kBatchWaves * 64, lds, s>>>(a, G, share);

@@ -528,10 +528,10 @@ hipError_t gemm_tiles(const MxGemmArgs& g, int K, hipStream_t s) {
 template <int TYPE, int FT>
 hipError_t gemm_few(const MxGemmArgs& g, int K, hipStream_t s) {
     const long long tiles_m = ((long long)g.M + 31) / 32, tiles = tiles_m * (((long long)g.T + 32 * FT - 1) / (32 * FT));
-    const int waves = std::min(tiles > 256 ? 4 : 8, mx_units(K));
+    const int waves = std::min(tiles > 256 ? 4 : kFewMaxWaves, mx_units(K));
     const size_t lds = (size_t)waves * (1 + FT) * 4096;
-    if (lds > 65536) {                                               // above what a launch gets without asking
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemm_few_kernel<TYPE, FT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (lds > 65536) {                                               // above what a launch gets without asking; always the most, as another thread may be between this and its launch
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemm_few_kernel<TYPE, FT>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewMaxWaves * (1 + FT) * 4096);
         if (e != hipSuccess) return e;
     }
     mx_gemm_few_kernel<TYPE, FT><<<dim3((unsigned)tiles), waves * 64, lds, s>>>(g, (int)tiles_m, K);

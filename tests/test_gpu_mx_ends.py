@@ -69,3 +69,38 @@ def test_quantisation_of_the_most_tiles():
     assert same_as_by_rows(columns, w)
     del columns, by_rows, w, row
     torch.cuda.empty_cache()
+
+
+def test_calls_from_two_threads():
+    """the same kernels with different needs of LDS, called by two host threads at once on streams of their own"""
+    import threading
+    import torch
+    import paper_2306_07629_amd as sq
+    rng = np.random.default_rng(3)
+    work = []
+    for M, T in ((20480, 40), (32768, 64)):
+        w = sq.mx_quantize(torch.from_numpy(rng.normal(size=(M, 2048)).astype(np.float16)).cuda())
+        few = sq.MxMatrix(M // 40, 2048, w.codes[:M // 40], w.scales[:M // 40])
+        x = torch.from_numpy(rng.normal(size=(2048, 16)).astype(np.float16)).cuda()
+        tokens = sq.mx_quantize(torch.from_numpy(rng.normal(size=(T, 2048)).astype(np.float16)).cuda())
+        work.append((w, x, tokens, few))
+    step = lambda w, x, tokens, few: (sq.mx_gemv(w, x), sq.mx_gemm(tokens, few, torch.float32))
+    want = [step(*k) for k in work]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def run(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(200):
+                    got[i] = step(*work[i])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:
+            errors.append(e)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    assert all(torch.equal(a, b) for i in range(2) for a, b in zip(got[i], want[i]))

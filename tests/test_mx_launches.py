@@ -33,3 +33,24 @@ def test_quantisation_along_the_columns(M, N, tiles, rows):
         assert all(is_possible(l, max([v for _, v in limits], default=0)) for l in launched), launched
         assert all(grid[0] % 8 == 0 for _, grid, _, _ in launched)
         assert sum(grid[0] for _, grid, _, _ in launched) == -(-tiles // 8) * 8
+
+
+def gemv(M, N, B):
+    return "sqllm_mx_gemv", "iiippppip", [M, N, B, A, A, A, A, 0, 0]
+
+
+def test_the_limit_of_lds_of_a_kernel_is_one_number():
+    """the limit belongs to the kernel, and a thread may set it between another's setting and that other's launch: whatever the sizes, every call sets the same"""
+    calls = [gemv(M, N, B) for B in (3, 7, 12, 16) for N in (2176, 5120, 8192, 28672) for M in (100, 4097, 12289, 16000, 20480, 32768, 100000)]
+    calls += [gemm(T, M, N, type) for type in range(3) for T in (1, 20, 33, 40, 64) for M in (40, 500, 1000) for N in (1500, 1664, 1792, 2048, 4096)]
+    calls += [quantize(200, 300, type, rows, True) for type in range(3) for rows in (False, True)]
+    limit, largest = {}, {}
+    for status, limits, launched in launches(calls):
+        assert status == 0
+        for kernel, size in limits:
+            limit.setdefault(kernel, set()).add(size)
+        for kernel, _, _, size in launched:
+            largest[kernel] = max(size, largest.get(kernel, 0))
+    assert len(limit) == 4 * 3 + 3 + 2, limit                            # column counts x shares of the gemv, types of the product of few rows, forms of the tile in fp32
+    assert all(len(sizes) == 1 for sizes in limit.values()), limit
+    assert all(largest[kernel] <= min(sizes) <= 160 * 1024 for kernel, sizes in limit.items())

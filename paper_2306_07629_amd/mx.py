@@ -91,6 +91,10 @@ class MxMatrix:
     @staticmethod
     def empty(M, N, device):
         _need_size(M, N)
+        return MxMatrix._empty(M, N, device)
+
+    @staticmethod
+    def _empty(M, N, device):
         padded = -(-N // ROW) * ROW
         m = object.__new__(MxMatrix)
         m.M, m.N = M, N
@@ -107,13 +111,15 @@ class MxMatrix:
         ty = _type_of(dtype)
         codes = self.codes
         out = _empty(self.M, self.N, dtype, codes.device)
+        if self.N == 0:
+            return out
         _call(codes.get_device(), DEQUANTIZE, self.M, self.N, ty, codes, self.scales, out, self.N)
         return out
 
 
 def mx_quantize(w: torch.Tensor, direction: str = "rows"):
     """w [M, N] packed with its blocks along the rows ("rows"), its transpose, an N x M matrix with blocks along the columns of w ("columns"), or
-    the pair of both from one pass over w ("both")."""
+    the pair of both from one pass over w ("both").  A matrix without rows or columns is packed as one: the sums over nothing that its products are are zeros."""
     if direction not in ("rows", "columns", "both"):
         raise ValueError(f"direction = {direction!r} is none of 'rows', 'columns' and 'both'")
     _need(w, "w")
@@ -121,9 +127,15 @@ def mx_quantize(w: torch.Tensor, direction: str = "rows"):
     w, ld = _rows(w, "w")
     M, N = w.shape
     device = w.device
-    rows = MxMatrix.empty(M, N, device) if direction != "columns" else None
-    columns = MxMatrix.empty(N, M, device) if direction != "rows" else None
-    _call(w.get_device(), QUANTIZE, M, N, ty, w, ld, rows and rows.codes, rows and rows.scales, columns and columns.codes, columns and columns.scales)
+    rows = columns = None
+    if direction != "columns":
+        _need_size(M, N or 1)
+        rows = MxMatrix._empty(M, N, device)
+    if direction != "rows":
+        _need_size(N, M or 1)
+        columns = MxMatrix._empty(N, M, device)
+    if M and N:
+        _call(w.get_device(), QUANTIZE, M, N, ty, w, ld, rows and rows.codes, rows and rows.scales, columns and columns.codes, columns and columns.scales)
     return (rows, columns) if direction == "both" else rows or columns
 
 
@@ -162,6 +174,10 @@ def mx_gemm(x: MxMatrix, w: MxMatrix, dtype=torch.float16, y: torch.Tensor | Non
         ld = y.stride(0) if x.M > 1 else w.M
         if w.M > 1 and y.stride(1) != 1 or ld < w.M:
             _refuse("SQLLM_ERR_SHAPE", f"y has strides {y.stride()}: its rows must be contiguous and must not overlap")
+    if w.N == 0:                                                     # sums over nothing
+        if not accumulate:
+            y.detach().zero_()
+        return y
     _call(codes.get_device(), GEMM, x.M, w.M, w.N, ty, x.codes, x.scales, codes, w.scales, y, ld, 1 if accumulate else 0)
     return y
 

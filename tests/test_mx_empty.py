@@ -1,0 +1,70 @@
+"""Packed matrices without rows or columns: an empty batch of tokens, or a layer without rows, through the calls of a training step."""
+import pytest
+import torch
+
+import paper_2306_07629_amd as sq
+from paper_2306_07629_amd import binding
+from test_mx_boundary import fake, status
+
+
+def shapes(m):
+    return m.M, m.N, tuple(m.codes.shape), tuple(m.scales.shape)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+def test_matrices_of_nothing_are_packed_without_a_launch(dtype):
+    rows, columns = sq.mx_quantize(fake(0, 300, dtype=dtype), "both")
+    assert shapes(rows) == (0, 300, (0, 192), (0, 12)) and shapes(columns) == (300, 0, (300, 0), (300, 0))
+    assert shapes(sq.mx_quantize(fake(0, 300, dtype=dtype), "columns")) == shapes(columns) and shapes(sq.mx_quantize(fake(0, 300, dtype=dtype))) == shapes(rows)
+    rows, columns = sq.mx_quantize(fake(5, 0, dtype=dtype), "both")
+    assert shapes(rows) == (5, 0, (5, 0), (5, 0)) and shapes(columns) == (0, 5, (0, 64), (0, 4))
+    assert rows.dequantize(dtype).shape == (5, 0)
+
+
+def test_a_size_beyond_the_librarys_is_refused_beside_none():
+    for w in (torch.empty((0, 1 << 31), dtype=torch.float16), torch.empty((1 << 31, 0), dtype=torch.float16)):
+        w = w.as_subclass(type(fake(1)))
+        for direction in ("rows", "columns", "both"):
+            if w.shape[0] and direction == "rows" or w.shape[1] and direction == "columns":
+                assert status(sq.mx_quantize, w, direction) == "SQLLM_ERR_SHAPE"
+        assert status(sq.mx_quantize, w, "both") == "SQLLM_ERR_SHAPE"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+def test_training_step_without_tokens(dtype):
+    M, N = 40, 300
+    w, w_t = sq.mx_quantize(torch.ones((M, N), dtype=dtype, device="cuda"), "both")
+    x = torch.zeros((0, N), dtype=dtype, device="cuda")
+    _, x_t = sq.mx_quantize(x, "both")
+    y = sq.mx_linear(x, w)
+    assert y.shape == (0, M) and y.dtype is dtype
+    dx, dw = sq.mx_linear_backward(torch.zeros_like(y), x_t, w_t)
+    assert dx.shape == (0, N) and dx.dtype is dtype
+    assert dw.shape == (M, N) and dw.dtype is torch.float32 and not bool(dw.any())
+    held = torch.full((M, N), 3.0, device="cuda")
+    dx, dw = sq.mx_linear_backward(torch.zeros_like(y), x_t, w_t, dw=held)
+    assert dw is held and bool((held == 3.0).all())
+
+
+@pytest.mark.gpu
+def test_training_step_of_a_layer_without_rows():
+    T, N = 7, 300
+    w, w_t = sq.mx_quantize(torch.zeros((0, N), dtype=torch.bfloat16, device="cuda"), "both")
+    x = torch.ones((T, N), dtype=torch.bfloat16, device="cuda")
+    _, x_t = sq.mx_quantize(x, "both")
+    y = sq.mx_linear(x, w)
+    assert y.shape == (T, 0)
+    dx, dw = sq.mx_linear_backward(torch.zeros_like(y), x_t, w_t)
+    assert dx.shape == (T, N) and not bool(dx.any()) and dw.shape == (0, N)
+
+
+@pytest.mark.gpu
+def test_sums_over_nothing_are_written_where_they_were_asked_for():
+    a, b = (sq.mx_quantize(torch.zeros((n, 0), dtype=torch.float16, device="cuda")) for n in (3, 5))
+    big = torch.full((3, 9), 2.0, dtype=torch.float16, device="cuda")
+    y = big[:, 2:7]
+    assert sq.mx_gemm(a, b, y=y, accumulate=True) is y and bool((big == 2.0).all())
+    assert sq.mx_gemm(a, b, y=y) is y and not bool(y.any()) and bool((big[:, :2] == 2.0).all()) and bool((big[:, 7:] == 2.0).all())
+    assert status(sq.mx_gemm, a, sq.mx_quantize(torch.zeros((5, 128), dtype=torch.float16, device="cuda"))) == "SQLLM_ERR_SHAPE"
+    assert status(sq.mx_gemv, a, torch.zeros((0, 1), dtype=torch.float16, device="cuda")) == "SQLLM_ERR_SHAPE"

@@ -189,9 +189,12 @@ def mx_linear(x: torch.Tensor, w: MxMatrix, dtype=None) -> torch.Tensor:
 
 def mx_linear_backward(dy: torch.Tensor, x_t: MxMatrix, w_t: MxMatrix, dtype=None, dw: torch.Tensor | None = None):
     """Gradients of y = Q(x) Q(w)^T (rounding passes gradients through) for dy [T, M]: dx = Q(dy) Q(w) in dtype (that of dy if None), and dw = Q(dy)^T Q(x)
-    in fp32, added to `dw` where that is given.  x_t and w_t are the packed transposes of x [T, N] and w [M, N]: mx_quantize(..., "both")[1].
+    in fp32, added to `dw` (fp32 too: sums of gradients are not rounded to fewer bits between steps) where that is given.  x_t and w_t are the packed
+    transposes of x [T, N] and w [M, N]: mx_quantize(..., "both")[1].
     The blocks of dy lie along the rows for dx and along the columns for dw, as the sums run."""
     _need(dy, "dy", w_t.codes, None, (x_t.N, w_t.N))
+    if dw is not None:
+        _need(dw, "dw", w_t.codes, torch.float32, (w_t.N, x_t.M))
     rows, columns = mx_quantize(dy, "both")
     dx = mx_gemm(rows, w_t, dy.dtype if dtype is None else dtype)
     if dw is None:

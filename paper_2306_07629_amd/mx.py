@@ -193,6 +193,8 @@ def mx_linear_backward(dy: torch.Tensor, x_t: MxMatrix, w_t: MxMatrix, dtype=Non
     transposes of x [T, N] and w [M, N]: mx_quantize(..., "both")[1].
     The blocks of dy lie along the rows for dx and along the columns for dw, as the sums run."""
     _need(dy, "dy", w_t.codes, None, (x_t.N, w_t.N))
+    if x_t.M != w_t.M:
+        _refuse("SQLLM_ERR_SHAPE", f"x has {x_t.M} columns, w has {w_t.M}")
     if dw is not None:
         _need(dw, "dw", w_t.codes, torch.float32, (w_t.N, x_t.M))
     rows, columns = mx_quantize(dy, "both")

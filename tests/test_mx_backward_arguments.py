@@ -10,7 +10,7 @@ T, M, N = 6, 5, 300
 
 @pytest.mark.parametrize("name,change", [("TYPE", dict(dw=fake(M, N, dtype=torch.float16))), ("TYPE", dict(dw=fake(M, N, dtype=torch.bfloat16))), ("TYPE", dict(dw=fake(M, N, dtype=torch.float64))),
                                          ("SHAPE", dict(dw=fake(N, M, dtype=torch.float32))), ("SHAPE", dict(dw=fake(M, N + 1, dtype=torch.float32))), ("DEVICE", dict(dw=torch.zeros(M, N))),
-                                         ("SHAPE", dict(x_t=packed(N, T + 1))), ("SHAPE", dict(w_t=packed(N, M + 1)))])
+                                         ("SHAPE", dict(x_t=packed(N + 1, T))), ("SHAPE", dict(x_t=packed(N, T + 1))), ("SHAPE", dict(w_t=packed(N, M + 1)))])
 def test_refused_before_dy_is_packed(name, change, monkeypatch):
     def launched(*args):
         raise AssertionError("reached the library")

@@ -512,8 +512,11 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
 
 namespace {
 
+constexpr int kTileShort = 512, kTileMost = 1 << 24;                 // columns: below, rows of SHORT's form; above, offsets inside a tile leave 32 bits
+
 template <int TYPE, int F, bool SHORT>
 hipError_t gemm_tiles(const MxGemmArgs& g, int K, hipStream_t s) {
+    if ((K < kTileShort) != SHORT || K > kTileMost) return hipErrorInvalidValue;   // the kernel would read scales or codes that are not there
     constexpr int R = TileShape<F>::kRows;
     const TileOrder order = {(int)(((long long)g.M + R - 1) / R), (int)(((long long)g.T + R - 1) / R), R};
     const unsigned grid = F == 4 ? 256 : 512;                        // one workgroup to a compute unit, or two
@@ -554,8 +557,8 @@ hipError_t gemm(const MxGemmArgs& g, hipStream_t s) {
     const int K = mx_padded(g.N);
     const int size = mx_type_size(TYPE);
     const double k = K / 1024.0, cost2 = cost_of_128(g.M, g.T, k, size), few = cost_of_few(g.M, g.T, k);
-    if (K <= 1 << 24) {                                              // offsets inside a tile are 32 bits
-        if (K < 512) {
+    if (K <= kTileMost) {
+        if (K < kTileShort) {
             if (cost2 < few) return gemm_tiles<TYPE, 2, true>(g, K, s);
         } else {
             const double cost4 = cost_of_256(g.M, g.T, k, size);

@@ -54,3 +54,17 @@ def test_the_limit_of_lds_of_a_kernel_is_one_number():
     assert len(limit) == 4 * 3 + 3 + 2, limit                            # column counts x shares of the gemv, types of the product of few rows, forms of the tile in fp32
     assert all(len(sizes) == 1 for sizes in limit.values()), limit
     assert all(largest[kernel] <= min(sizes) <= 160 * 1024 for kernel, sizes in limit.items())
+
+
+def test_tiles_take_the_rows_they_are_made_for():
+    """below 512 columns a row has fewer scales than the other form of the tiles reads at once; above 2^24 its offsets leave 32 bits"""
+    calls = [gemm(T, M, N, type) for type in range(3) for T in (1, 33, 300, 4096, 20000) for M in (1, 64, 1000, 22016) for N in (1, 128, 129, 384, 385, 512, 640, 8192, 1 << 24, (1 << 24) + 1, 1 << 28)]
+    short, plain, few = 0, 0, 0
+    for (_, _, args), (status, _, launched) in zip(calls, launches(calls)):
+        K = -(-args[2] // 128) * 128
+        assert status == 0 and len(launched) == 1
+        kernel = launched[0][0]
+        if "tile" in kernel:
+            assert ("ELb1E" in kernel) == (K < 512) and ("ELb0E" in kernel) == (K >= 512) and K <= 1 << 24, (args, kernel)
+        short, plain, few = short + ("ELb1E" in kernel), plain + ("ELb0E" in kernel), few + ("few" in kernel)
+    assert short and plain and few

@@ -68,3 +68,9 @@ def test_tiles_take_the_rows_they_are_made_for():
             assert ("ELb1E" in kernel) == (K < 512) and ("ELb0E" in kernel) == (K >= 512) and K <= 1 << 24, (args, kernel)
         short, plain, few = short + ("ELb1E" in kernel), plain + ("ELb0E" in kernel), few + ("few" in kernel)
     assert short and plain and few
+
+
+@pytest.mark.parametrize("T,M,N,kernel", [(20, 70, 4100, "few_kernelILi{}ELi1E"), (300, 270, 1152, "few_kernelILi{}ELi2E"), (1030, 2050, 300, "ELb1E"), (2100, 4100, 640, "Li2ELNS"), (4090, 4000, 4900, "Li4ELNS")])
+def test_the_sizes_of_the_range_tests_take_every_kernel(T, M, N, kernel):
+    for type in range(3):
+        assert kernel.format(type) in launches([gemm(T, M, N, type)])[0][2][0][0]

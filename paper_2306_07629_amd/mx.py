@@ -1,5 +1,8 @@
 """Matrices of microscaled 4-bit floating point: thin binding of the sqllm_mx_* entry points.  Checks shapes, allocates outputs, marshals the
-arguments (no arithmetic here); every call enqueues on the current stream of its tensors' device."""
+arguments (no arithmetic here); every call enqueues on the current stream of its tensors' device.
+
+No call here is recorded by autograd: operands may require gradients, results never do, and what is written to a given `y` or `dw` autograd does not
+see.  The gradients of a layer are mx_linear_backward's, which a program calls itself, for instance in a torch.autograd.Function of its own."""
 from __future__ import annotations
 
 import torch
@@ -140,7 +143,8 @@ def mx_quantize(w: torch.Tensor, direction: str = "rows"):
 
 
 def mx_gemv(w: MxMatrix, x: torch.Tensor, y: torch.Tensor | None = None, accumulate: bool = False) -> torch.Tensor:
-    """W x for fp16 x [N, B], B = 1..16, as fp16 [M, B]; with accumulate, y + W x in y"""
+    """W x for fp16 x [N, B], B = 1..16, as fp16 [M, B]; with accumulate, y + W x in y.  N is a multiple of 128, at most 28672, and x starts at a multiple of 16 bytes
+    (mx_linear takes any N and any x); no gradient is recorded"""
     codes, B = w.codes, x.shape[1] if x.dim() == 2 else 0
     _need(x, "x", codes, torch.float16, (w.N, B))
     if y is None:
@@ -183,7 +187,7 @@ def mx_gemm(x: MxMatrix, w: MxMatrix, dtype=torch.float16, y: torch.Tensor | Non
 
 
 def mx_linear(x: torch.Tensor, w: MxMatrix, dtype=None) -> torch.Tensor:
-    """y = Q(x) W^T for tokens x [T, N] and a packed layer W [M, N], [T, M] in dtype (that of x if None)"""
+    """y = Q(x) W^T for tokens x [T, N] and a packed layer W [M, N], [T, M] in dtype (that of x if None); no gradient is recorded (mx_linear_backward)"""
     return mx_gemm(mx_quantize(x), w, x.dtype if dtype is None else dtype)
 
 

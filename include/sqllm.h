@@ -40,8 +40,8 @@
  *
  * ERRORS  every function returns an sqllm_status.  Arguments are validated on the host first and nothing is enqueued
  *   when validation fails.  An entry point that needs several kernel launches (batches of the one-thread-per-row
- *   kernel beyond 8 columns, more than 2^22 rows in the parity exports, the offline pass) can fail in a later
- *   launch with SQLLM_ERR_HIP after earlier ones were enqueued; its outputs are then undefined.  A text for the last
+ *   kernel beyond 8 columns, more than 2^22 rows in the parity exports, the offline pass, sqllm_mx_gemv beyond 2^28 rows, sqllm_mx_quantize beyond 2^23
+ *   tiles of 128 x 128 with codes_t) can fail in a later launch with SQLLM_ERR_HIP after earlier ones were enqueued; its outputs are then undefined.  A text for the last
  *   error of the calling thread is available from sqllm_last_error_string().
  *   M == 0 -> SQLLM_OK, nothing enqueued.  N must be positive: N == 0 (an empty sum) is SQLLM_ERR_SHAPE, the caller
  *   clears y itself.  The library holds gfx950 code only: on any other device the first call that would launch
@@ -227,7 +227,8 @@ int sqllm_quantize_layer_noalloc(int M, int N, int bits, int max_iter, const voi
  * A packed matrix of M rows and N columns is two device arrays.  Its rows are padded to P = 128 ceil(N / 128) columns.
  *   codes   uint8 [M][P / 2]   column j of a row in the low (j even) or high (j odd) four bits of byte j / 2: bit 3 is the sign, bits 2..0 name
  *                              the magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (two exponent bits, one fraction bit); columns N .. P - 1 hold zeros
- *   scales  uint8 [M][P / 32]  one byte s per block of 32 neighbouring columns, the factor 2^(s - 127); 255 makes the block NaN
+ *   scales  uint8 [M][P / 32]  one byte s per block of 32 neighbouring columns, the factor 2^(s - 127); 255 makes the block NaN (also a block of the padding alone,
+ *                              which sqllm_mx_quantize gives 0)
  * codes are 16-byte aligned, scales 4-byte.  Unpacked matrices are row-major with a row stride ld (in elements, at least the number of columns), aligned
  * to their element; 16-byte aligned rows are faster.  N is any number of columns from 1 to 2^31 - 128 unless stated otherwise, M any number of rows; M == 0 -> SQLLM_OK.
  *
@@ -239,12 +240,16 @@ int sqllm_quantize_layer_noalloc(int M, int N, int bits, int max_iter, const voi
  *                      Either pair may be NULL, not both; w is read once for both.  Rounding and scales are exact: the result is a pure function of w.
  * sqllm_mx_dequantize  writes code * 2^(s - 127) as `type` to w_out [M][N], stride ldw; rounded once (fp16: beyond 65504 to Inf; exact where the type holds the value).
  * sqllm_mx_gemv        y = W x (accumulate == 0) or y = fp16( fp32(y) + W x ): x fp16 [N][B], y fp16 [M][B], B = 1..16, N and the alignments of x and y as for sqllm_lut_gemv, so that
- *                      sqllm_csr_spmv can add a sparse term of the same layer to y.  Products are exact, sums in fp32.  An Inf or NaN of x makes its column of y, and no other, Inf or NaN.
+ *                      sqllm_csr_spmv can add a sparse term of the same layer to y.  Sums in fp32 of exact products, but that with B >= 3 the blocks with s <= 60 may count as
+ *                      zeros: together they add less than 28672 x 65504 x 6 x 2^-67 < 2^-32 to a result, half the smallest fp16 number being 2^-25.  An Inf or NaN of x makes
+ *                      its column of y, and no other, Inf or NaN.
  * sqllm_mx_gemm        y[t][i] = sum_j X[t][j] W[i][j] of two packed matrices: X has T rows, W has M, both N columns; y is `type` [T][M] with row stride ldy.  accumulate != 0 adds to
- *                      what y holds (read as `type`, added in fp32).  Products are exact, sums in fp32; one rounding to `type`.  T == 0 -> SQLLM_OK.
+ *                      what y holds (read as `type`, added in fp32).  Products and sums in fp32: a product is exact where fp32 holds it (the scales reach from 2^-254 to 2^254: it
+ *                      rounds to a multiple of 2^-149, or becomes Inf); one rounding to `type`.  T == 0 -> SQLLM_OK.
  *                      With X the tokens and W a layer this is its forward pass.  Backward, with dY [T][M]: dX = sqllm_mx_gemm of dY's rows and W's transpose, dW = of dY's transpose and X's transpose.
  * Outputs must not overlap inputs.  Nothing but the named elements is written (rows of y and w_out keep what lies between their end and the next row).
- * A NaN scale reaches every element of y whose sum it is part of.  Results do not depend on the launch: no atomics, fixed order of additions for a given shape.                     */
+ * A NaN scale reaches every element of y whose sum it is part of.  Results do not depend on the launch: no atomics, fixed order of additions for a given shape (and, with B >= 3 in
+ * sqllm_mx_gemv, for given scales of the 16 rows 16 i .. 16 i + 15 that a row is one of: scales that leave fp16 send them to another order).                                         */
 int sqllm_mx_bytes(int M, int N, size_t* code_bytes, size_t* scale_bytes);
 int sqllm_mx_quantize(int M, int N, int type, const void* w, long long ldw, void* codes, void* scales,
                       void* codes_t, void* scales_t, void* stream);

@@ -8,7 +8,7 @@
 namespace sqllm {
 
 constexpr int kMxBlock = 32;        // elements that share a scale
-constexpr int kMxRowUnit = 128;     // elements a packed row is padded to: one step of the matrix instructions
+constexpr int kMxRowUnit = 128;     // elements a packed row is padded to: four blocks, whose scales are a dword, and one to four matrix instructions
 constexpr int kMxMaxN = 0x7FFFFF80; // longest row: its padded length is still an int
 
 inline int mx_padded(int n) { return (int)(((long long)n + kMxRowUnit - 1) / kMxRowUnit * kMxRowUnit); }

@@ -87,7 +87,8 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxDequantArgs a
 // asked for too, are quantised on the way, so w is read once for both), then every thread walks down 32 rows of a column, or of two.  Codes and
 // scales of the columns, and scales of the rows, are gathered in LDS and leave four neighbouring bytes, or sixteen, to a lane: a byte of a row of
 // its own from every lane took longer (5120 x 5120 fp16, both directions: 28.0
-// against 24.8 us; with the loads past the caches 21.8).
+// against 24.8 us; with the loads past the caches 21.8).  Within a sixth of the copy rate for 4096 x 11008 (bf16 32.9 us, fp32, of whose tiles two fit a compute unit, 51.2);
+// below some tiles to a compute unit one tile's chain shows (1999 x 5120: 10.3 for 6.4 us in bf16, 16.4 for 10.6 in fp32).
 constexpr int kTile = 128;
 
 template <int TYPE, bool ROWS>
@@ -182,7 +183,8 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_tile_kernel(MxQuantArgs 
 // One or two columns: wave w of a workgroup owns columns [2048 w, 2048 w + 2048) of W, lane l block 64 w + l of every row, and keeps the 32 rows of x of
 // its block in 16 registers per column of x while it walks down the workgroup's rows, R at a time with the next R requested.  The codes are converted
 // without their scale (every code is an fp16 number), so a block's sum is formed as for fp16 weights, and enters the row's sum times the scale in
-// fp32: no scale byte leaves a range.
+// fp32: no scale byte leaves a range.  Bound by reads: 22016 x 8192 from HBM 21.6 us (4.4 TB/s; its bytes at the rate of a copy 19.6), from a warm last-level cache 20.1; two
+// columns, with twice the dot products to a row's bytes, 25.5 and 24.6.
 template <int R>
 struct BlockRows {
     u32x4 codes[R];
@@ -313,7 +315,8 @@ __global__ void __launch_bounds__(kGemvMaxWaves * 64) mx_gemv_kernel(MxGemvArgs 
 // Lane (r, q) takes block q of row r of every step, converted with its scale to fp16, eights 0..3 for instructions 0..3; the scales of a step are fetched
 // four lanes to a row and change lanes when they are used.  The wave's rows of x are read once per round, go through the wave's own LDS (padded there to a multiple of four columns) to
 // be transposed, and stay in 16 NS registers while the wave walks down the groups of 16 rows, RING of them ahead of itself with its requests.
-// What columns past B hold reaches columns that are not stored.
+// What columns past B hold reaches columns that are not stored.  8192 x 8192 times 16 takes 15.4 us with weights from HBM and 11.4 from the last-level cache, times 3 13.2
+// and 8.9 (the bytes at the rate of a copy: 7.4): launch and x in place, then reads.
 //
 // With its scale a code is an fp16 number for scale bytes 114 .. 140 (0.5 x 2^-13 .. 6 x 2^13).  A block with a byte of 60 or less adds less than
 // 28672 x 65504 x 6 x 2^(60 - 127) < 2^-32 to any result, far below half the smallest fp16 number, and becomes zeros.  Other bytes
@@ -394,7 +397,7 @@ __global__ void __launch_bounds__(kBatchWaves * 64, 2) mx_gemv_batch_kernel(MxGe
         const int first = min((round * kBatchWaves + wave) * share, total);   // the wave's first step
         const int n = min(share, total - first);                     // uniform; may be 0
         long long top = r0;
-        asm volatile("" : "+s"(top));                                // rows' addresses made anew each round: kept, they were spilled, and waited for x on their way back (8192 x 8192 times 5: 15.3 us, now 13.4)
+        asm volatile("" : "+s"(top));                                // rows' addresses made anew each round: kept, they were spilled, and waited for x on their way back (8192 x 8192 times 5, weights from HBM: 15.3 us, now 13.4)
         auto fetch = [&](int g, BatchCodes<NS>& d) {
             const size_t row = (size_t)min(top + 16 * g + r, (long long)a.M - 1);
             const u32x4* codes = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.codes) + row * (a.N / 2)) + 4 * first + q;
@@ -410,7 +413,7 @@ __global__ void __launch_bounds__(kBatchWaves * 64, 2) mx_gemv_batch_kernel(MxGe
         half8_t xb[NS][4];
         {
             // x: lane l fetches rows 2 l and 2 l + 1 of a step (B dwords); rows of 4, 8, 12 or 16 need no padding, and the step goes to LDS as it lies, sixteen
-            // neighbouring bytes to a lane (8192 x 8192 times 16: 17.1 us, now 15.4; 4096 x 14336 20.7, now 16.7)
+            // neighbouring bytes to a lane (weights from HBM: 8192 x 8192 times 16 17.1 us, now 15.4; 4096 x 14336 20.7, now 17.0)
             constexpr bool kWhole = P == B;
             const u32* x = static_cast<const u32*>(a.x) + (size_t)B * (64 * min(first, total - 1) + lane);
             constexpr int C = NS * B <= 36 ? NS : 4, EARLY = NS == 8 ? 1 : RING;   // steps of x requested ahead, groups of codes before x is in place: what 256 registers hold

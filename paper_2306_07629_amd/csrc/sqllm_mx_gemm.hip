@@ -134,11 +134,16 @@ __global__ void __launch_bounds__(kFewMaxWaves * 64, 2) mx_gemm_few_kernel(MxGem
 // bytes of a row to eight lanes, whole cache lines), writes the next stage to the LDS buffer that is not being read, and feeds the matrix
 // instructions from the other; one barrier a stage.  Operands are read a step (64 columns) ahead.  Scales go the same way in groups of 1024 columns, half
 // the rows every second stage: a request is an access of the vector L1 for every row it touches, so two lanes take 32 bytes of a row (in groups of 512, a lane
-// to a row, 2047 x 4096 x 11008 took 74 us, now 69).  Chunk c (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor
+// to a row, 2047 x 4096 x 11008 took 7 % longer).  Chunk c (16 bytes) of row r lies at position c ^ g(r) of the row's 128 bytes, so that neither 8 nor
 // 16 neighbouring lanes, which read the same chunk of different rows, meet in a bank.
 //
-// What bounds it: the matrix instructions alone, operands of random data in registers, make 6.6 PFLOP/s on this card at the clock its power allows (9.8 on
-// zeros); here 3.4 (4.1 on zeros).  Left out one by one (zeros): scales' way to LDS a tenth, codes' way to LDS a tenth, their requests a sixth of the time.
+// What bounds it (4096 x 22016 x 8192 to bf16: 434 us, 3.4 PFLOP/s): 850 000 cycles, on zeros as on random data, in 41 % of which the matrix pipes are busy; with one
+// wave to a SIMD the traffic through LDS, the requests and the results take the rest.  Power takes the clock from 2.35 GHz (zeros: 363 us) to 1.97.  The
+// instructions alone, operands in registers, make 6.6 PFLOP/s on random data and 9.8 on zeros.  Left out one by one (zeros): scales' way to LDS a tenth, codes' way
+// to LDS a tenth, their requests a sixth of the time.
+//
+// Registers: the 256-row forms need all 512 and spill 47 to 76 more (and 37 to 109 scalar ones, to vector registers).  In those that write, every reload lies outside the loop
+// over the stages; in those that add to y, four or five lie in it, one set for each two stages.  The 128-row forms spill no vector registers.
 template <int F>
 struct TileShape {
     static constexpr int kRows = 64 * F;                             // of W and of X
@@ -188,7 +193,7 @@ __device__ __forceinline__ void add_rows(const MxGemmArgs& g, const char* lds, i
             else *reinterpret_cast<u32x4_a4*>(y) = __builtin_bit_cast(u32x4, v);
         }
     } else {
-        constexpr int kAhead = 8;                                    // rows read before the first is written (one: 4096 x 8191 of 1024 in fp32 169 us, now 93)
+        constexpr int kAhead = 8;                                    // rows read before the first is written (one: 4096 x 8191 of 1000 in fp32, y from HBM, 169 us, now 92; bytes 56)
         for (int i = 0; i < R / 8; i += kAhead) {
             const int row0 = R / 8 * wave + i;
             value* const y = static_cast<value*>(g.y) + (t0 + row0) * g.ldy + m0;
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
             for (int k = 0; k < F; ++k) acc[i][k] = mma<decltype(s)::value>(a[i], b[k], acc[i][k], ua[i], ub[k]);
     };
     // The order of a step's instructions: the reads of the next step's operands as early as they fit, a write to LDS and a request between two matrix
-    // instructions (reads spread over the whole step: 301 x 5120 x 5120 16.0 us, now 15.5; 4096 x 22016 x 8192 454, now 448).
+    // instructions (reads spread over the whole step take 3 % longer at 301 x 5120 x 5120, 1.3 % at 4096 x 22016 x 8192).
     auto arrange = [&](auto group, auto writes) {
         constexpr int G = decltype(group)::value;
         if constexpr (F == 2) {
@@ -440,7 +445,7 @@ __global__ void __launch_bounds__(256, F == 4 ? 1 : 2) mx_gemm_tile_kernel(MxGem
         }
         if constexpr (OUT != kAdd) {
             // Four lanes exchange their 64 bytes of four rows, so that each instruction writes eight whole lines, with no barrier and while the next
-            // tile's stage is on its way (4096 x 22016 results of 8192 columns: 442 us, 470 through LDS).
+            // tile's stage is on its way (4096 x 22016 results of 8192 columns: 6 % longer through LDS).
             const int c = lane & 3;
             typedef typename MxType<TYPE>::value value;
             typedef value pair __attribute__((ext_vector_type(2)));

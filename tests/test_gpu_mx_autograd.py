@@ -56,3 +56,18 @@ def test_a_layer_with_gradients():
         # dw is rounded to fp32 before fp16: half a step of fp32 more
         S = np.abs(a) @ np.abs(b).T
         close(host(got), a @ b.T, S, a.shape[1], extra=2.0 ** -24 * S)
+
+
+@pytest.mark.parametrize("T,M", [(1, 1), (1, 130), (70, 1), (70, 130)])
+def test_a_broadcast_gradient(T, M):
+    """what y.sum().backward() hands on: one number with strides of zero"""
+    import torch
+    import paper_2306_07629_amd as sq
+    x, w = leaf((T, 300), 1).detach(), leaf((M, 300), 2).detach()
+    x_t, w_t = sq.mx_quantize(x, "columns"), sq.mx_quantize(w, "columns")
+    one = torch.ones((), dtype=torch.float16, device="cuda").expand(T, M)
+    got = sq.mx_linear_backward(one, x_t, w_t)
+    want = sq.mx_linear_backward(one.clone(memory_format=torch.contiguous_format), x_t, w_t)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    near = host(x_t.dequantize(torch.float32)).sum(axis=1)
+    close(host(got[1]), np.broadcast_to(near, (M, 300)), np.broadcast_to(np.abs(host(x_t.dequantize(torch.float32))).sum(axis=1), (M, 300)), T, "f32")
